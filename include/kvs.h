@@ -44,6 +44,7 @@ extern "C" {
 #define KVS_VERSION 300          /* major*10000 + minor*100 + patch */
 #define KVS_MAX_Q_ROWS 1024      /* largest supported G*W */
 #define KVS_MAX_DECODE_ROWS 64   /* largest G*W of kvs_decode_attention */
+#define KVS_MAX_WINDOW_ROWS (1 << 22)   /* largest G*W of kvs_window_attention and its _packed form */
 #define KVS_MAX_LEN (1 << 22)    /* largest supported cache length of one unit, in tokens */
 #define KVS_STATIC_SCRATCH_BYTES (16u << 20)   /* workspace that kvs_step_static brings along, per GPU */
 
@@ -258,6 +259,59 @@ kvs_status kvs_step_per_query_counts(const kvs_problem* p, const void* Q, const 
                                      const int32_t* counts_in, void* K_out, void* V_out, int32_t* counts_out,
                                      int32_t* slot_of_token_out, uint8_t* edge_mask_out,
                                      void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Attention with a causal mask, a sliding window and first rows that stay visible, over a plain or merged cache: what a
+ * model's layer computes for the tokens that a step adds (a chunk of new tokens on a merged cache and itself, Sec. 3.1; a
+ * prompt; one new token, or several drafted ones, per query head).  Row t of a unit is a token, or a slot (k', V', c) of a
+ * merged cache as in kvs_decode_attention.  With causal = 1 the W queries of a head are those of the last W positions, the
+ * query at window position w being row len - W + w itself; with causal = 0 all of them are at the last row.  A query at
+ * position x sees the rows t <= x of which t < n_sink (Sec. 5: the first tokens) or, with span > 0, t > x - span; span = 0: all
+ * t <= x.  Then
+ *   out[u, g, w, :] = sum_t exp(e_t) V[t] / sum_t counts[t] exp(e_t)  over the rows that it sees,  e_t = scale * Q[u, g, w] . K[t]
+ * and zeros for a query that sees no row.  What a query does not see has no part in its result, whatever it holds (NaN and
+ * infinities too).  Unlike the calls above, these take units of no rows (len = 0) and, with causal = 1, units shorter than
+ * the window: queries before the unit's first row see nothing, so that prompts of unequal lengths may be padded in front.
+ * Units' row ranges may overlap (a prefix that several sequences share).  budget, out_row, n_recent and key_rule are not read
+ * (budget and out_row may be NULL); G*W <= KVS_MAX_WINDOW_ROWS.
+ *   span    rows that a query sees up to and including its own, 0: all (KVS_ERR_INVALID_ARG below 0)
+ *   Q       DEVICE in  [n_units, G, W, D] io_dtype
+ *   K, V    DEVICE in  [rows, D] io_dtype
+ *   counts  DEVICE in  [rows] i32, every entry >= 1, or NULL for a cache of plain tokens
+ *   out     DEVICE out [n_units, G, W, D] io_dtype: sums in fp32, rounded once; with KVS_BF16 the weights exp(e_t) enter the
+ *           product with V as bf16 numbers or sums of two of them, with KVS_F32 as sums of three or as they are
+ *   ws      DEVICE workspace of kvs_window_attention_workspace_size(p, span) bytes, 256-byte aligned; NULL is fine where that
+ *           is 0 (KVS_ERR_WORKSPACE).  It serves both forms.
+ * Asynchronous on hip_stream; nothing is allocated; errors are found on the host before any launch.                       */
+kvs_status kvs_window_attention_workspace_size(const kvs_problem* p, int32_t span, size_t* bytes);
+kvs_status kvs_window_attention(const kvs_problem* p, int32_t span, const void* Q, const void* K, const void* V,
+                                const int32_t* counts, void* out, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* A cache in 4 bits.  A row of D values is D / 32 blocks of 32 neighbouring channels.  A block is a scale byte s, which stands
+ * for 2^(s - 127), and 32 codes of 4 bits: bit 3 the sign, bits 0..2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Codes are D / 2 bytes a
+ * row, the lower channel in the lower nibble, scales D / 32 bytes a row; both [rows] like K and V (4.25 bits per value).
+ * kvs_pack writes the rows of a cache into such a one: s is the smallest with which no value of the block rounds beyond 6, at
+ * least 2 and at most 252 (a block of larger values than 6 * 2^125 is clamped to it); values round to the nearest, ties to even
+ * mantissas.  A block with an infinity or a NaN gets s = 255 and stands for NaNs.  kvs_unpack writes the values that codes and
+ * scales stand for, exactly, as io_dtype, so that the merge step can go on from a cache in 4 bits.
+ * Unit u's rows in_row[u] .. in_row[u] + len[u] of the source go to rows out_row[u] .. out_row[u] + len[u] of the destination
+ * (all of them: budget is not read); other rows of the destination keep what they hold, so that a step's new rows can be
+ * appended.  len = 0 is allowed; destination ranges must be disjoint (KVS_ERR_INVALID_ARG), source ranges need not be.  Of the
+ * problem only n_units, head_dim, io_dtype, len, in_row and out_row are read.
+ * KVS_ERR_DEVICE also where the host has no memory to check ranges that are in no ascending order.
+ *   K, V                DEVICE [rows, D] io_dtype
+ *   K_codes, V_codes    DEVICE [rows, D / 2] bytes
+ *   K_scales, V_scales  DEVICE [rows, D / 32] bytes
+ * No workspace; asynchronous on hip_stream; errors are found on the host before any launch.                              */
+kvs_status kvs_pack(const kvs_problem* p, const void* K, const void* V, void* K_codes, void* K_scales, void* V_codes,
+                    void* V_scales, void* hip_stream);
+kvs_status kvs_unpack(const kvs_problem* p, const void* K_codes, const void* K_scales, const void* V_codes,
+                      const void* V_scales, void* K, void* V, void* hip_stream);
+
+/* kvs_window_attention over a cache in 4 bits as kvs_pack leaves it (scales 2..252 and 255), read as it lies.  io_dtype is the
+ * type of Q and out.  Everything else is as there.                                                                       */
+kvs_status kvs_window_attention_packed(const kvs_problem* p, int32_t span, const void* Q, const void* K_codes,
+                                       const void* K_scales, const void* V_codes, const void* V_scales,
+                                       const int32_t* counts, void* out, void* ws, size_t ws_bytes, void* hip_stream);
 
 const char* kvs_status_str(kvs_status s);
 int kvs_version(void);

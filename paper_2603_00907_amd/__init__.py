@@ -25,6 +25,7 @@ from .binding import (  # noqa: F401
     kvs_merge_compact_counts,
     kvs_merge_compact_norms,
     kvs_merge_compact_norms_counts,
+    kvs_pack,
     kvs_per_query_workspace_size,
     kvs_score,
     kvs_score_counts,
@@ -36,6 +37,10 @@ from .binding import (  # noqa: F401
     kvs_step_per_query,
     kvs_step_per_query_counts,
     kvs_step_static,
+    kvs_unpack,
+    kvs_window_attention,
+    kvs_window_attention_packed,
+    kvs_window_attention_workspace_size,
     kvs_debug_set,
     kvs_debug_get,
     DEBUG_SWITCHES,

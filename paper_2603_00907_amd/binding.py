@@ -24,7 +24,8 @@ EXPORTS = ["kvs_workspace_size", "kvs_score", "kvs_select", "kvs_merge_compact",
            "kvs_score_counts", "kvs_merge_compact_counts", "kvs_step_counts", "kvs_decode_workspace_size",
            "kvs_decode_attention", "kvs_per_query_workspace_size", "kvs_sensitivity", "kvs_merge_compact_norms",
            "kvs_step_per_query", "kvs_sensitivity_counts", "kvs_merge_compact_norms_counts",
-           "kvs_step_per_query_counts", "kvs_step_static", "kvs_status_str", "kvs_version", "kvs_debug_set",
+           "kvs_step_per_query_counts", "kvs_step_static", "kvs_window_attention_workspace_size", "kvs_window_attention",
+           "kvs_window_attention_packed", "kvs_pack", "kvs_unpack", "kvs_status_str", "kvs_version", "kvs_debug_set",
            "kvs_debug_get"]
 
 STATIC_SCRATCH_BYTES = 16 << 20
@@ -91,14 +92,20 @@ def load_library(path: Optional[str] = None):
     lib.kvs_merge_compact_norms_counts.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.kvs_step_per_query_counts.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.kvs_step_static.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.kvs_window_attention_workspace_size.argtypes = [P, C.c_int32, C.POINTER(sz)]
+    lib.kvs_window_attention.argtypes = [P, C.c_int32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.kvs_window_attention_packed.argtypes = [P, C.c_int32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.kvs_pack.argtypes = [P, vp, vp, vp, vp, vp, vp, vp]
+    lib.kvs_unpack.argtypes = [P, vp, vp, vp, vp, vp, vp, vp]
     lib.kvs_debug_set.argtypes = [C.c_int, C.c_int]
     lib.kvs_debug_get.argtypes = [C.c_int]
     for name in ("kvs_workspace_size", "kvs_score", "kvs_select", "kvs_merge_compact", "kvs_step",
                  "kvs_score_counts", "kvs_merge_compact_counts", "kvs_step_counts", "kvs_decode_workspace_size",
                  "kvs_decode_attention", "kvs_per_query_workspace_size", "kvs_sensitivity",
                  "kvs_merge_compact_norms", "kvs_step_per_query", "kvs_sensitivity_counts",
-                 "kvs_merge_compact_norms_counts", "kvs_step_per_query_counts", "kvs_step_static", "kvs_debug_set",
-                 "kvs_debug_get"):
+                 "kvs_merge_compact_norms_counts", "kvs_step_per_query_counts", "kvs_step_static",
+                 "kvs_window_attention_workspace_size", "kvs_window_attention", "kvs_window_attention_packed", "kvs_pack",
+                 "kvs_unpack", "kvs_debug_set", "kvs_debug_get"):
         getattr(lib, name).restype = C.c_int
     lib.kvs_status_str.argtypes = [C.c_int]
     lib.kvs_status_str.restype = C.c_char_p
@@ -300,6 +307,38 @@ def kvs_step_static(problem: Problem, Q, K, V, counts_in, K_out, V_out, counts_o
     _check(load_library().kvs_step_static(
         problem.ref, _ptr(Q), _ptr(K), _ptr(V), _ptr(counts_in), _ptr(K_out), _ptr(V_out), _ptr(counts_out),
         _ptr(slot_of_token_out), _ptr(edge_mask_out), stream), "kvs_step_static")
+
+
+def kvs_window_attention_workspace_size(problem: Problem, span: int = 0) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().kvs_window_attention_workspace_size(problem.ref, span, C.byref(out)),
+           "kvs_window_attention_workspace_size")
+    return int(out.value)
+
+
+def kvs_window_attention(problem: Problem, Q, K, V, counts, out, ws=None, span: int = 0, stream: int = 0,
+                         ws_bytes: Optional[int] = None):
+    _check(load_library().kvs_window_attention(
+        problem.ref, span, _ptr(Q), _ptr(K), _ptr(V), _ptr(counts), _ptr(out), _ptr(ws),
+        (_nbytes(ws) if ws is not None else 0) if ws_bytes is None else ws_bytes, stream), "kvs_window_attention")
+
+
+def kvs_window_attention_packed(problem: Problem, Q, K_codes, K_scales, V_codes, V_scales, counts, out, ws=None,
+                                span: int = 0, stream: int = 0, ws_bytes: Optional[int] = None):
+    _check(load_library().kvs_window_attention_packed(
+        problem.ref, span, _ptr(Q), _ptr(K_codes), _ptr(K_scales), _ptr(V_codes), _ptr(V_scales), _ptr(counts), _ptr(out),
+        _ptr(ws), (_nbytes(ws) if ws is not None else 0) if ws_bytes is None else ws_bytes, stream),
+        "kvs_window_attention_packed")
+
+
+def kvs_pack(problem: Problem, K, V, K_codes, K_scales, V_codes, V_scales, stream: int = 0):
+    _check(load_library().kvs_pack(problem.ref, _ptr(K), _ptr(V), _ptr(K_codes), _ptr(K_scales), _ptr(V_codes),
+                                   _ptr(V_scales), stream), "kvs_pack")
+
+
+def kvs_unpack(problem: Problem, K_codes, K_scales, V_codes, V_scales, K, V, stream: int = 0):
+    _check(load_library().kvs_unpack(problem.ref, _ptr(K_codes), _ptr(K_scales), _ptr(V_codes), _ptr(V_scales), _ptr(K),
+                                     _ptr(V), stream), "kvs_unpack")
 
 
 def kvs_debug_set(which, value: int) -> int:

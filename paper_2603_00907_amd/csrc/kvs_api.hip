@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "kvs_device.h"
+#include "kvs_host.h"
 
 namespace kvs {
 
@@ -70,9 +71,6 @@ struct SwitchInit {
 int debug_switch(kvs_debug_switch which) { return g_switch[which].load(std::memory_order_relaxed); }
 
 namespace {
-
-constexpr size_t kAlign = 256;
-inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct Plan {
   int n_units = 0;
@@ -456,29 +454,7 @@ hipError_t per_query_norms(const Plan& plan, const UnitTable& tab, const Shape& 
   return launch_per_query_norms(tab, sh2, Q, K, V, counts_in, w.c_row, q.o_part, q.o_hi, q.o_lo, q.oo, a_tok, c_edge, s);
 }
 
-struct Range {
-  const void* p;
-  size_t bytes;
-  bool is_output;
-};
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-kvs_status check_ranges(const std::vector<Range>& rs) {
-  for (const Range& r : rs) {
-    if (r.p == nullptr || !aligned16(r.p)) return KVS_ERR_INVALID_ARG;
-  }
-  for (size_t i = 0; i < rs.size(); ++i) {
-    if (!rs[i].is_output) continue;
-    for (size_t j = 0; j < rs.size(); ++j) {
-      if (i == j) continue;
-      const char* a0 = (const char*)rs[i].p;
-      const char* b0 = (const char*)rs[j].p;
-      if (a0 < b0 + rs[j].bytes && b0 < a0 + rs[i].bytes) return KVS_ERR_ALIAS;
-    }
-  }
-  return KVS_OK;
-}
+kvs_status check_ranges(const std::vector<Range>& rs) { return check_ranges(rs.data(), rs.size()); }
 
 kvs_status check_ws(const Plan& plan, const void* ws, size_t ws_bytes, Workspace* out, void* ws_mut) {
   if (ws == nullptr || ((uintptr_t)ws % kAlign) != 0) return KVS_ERR_WORKSPACE;

@@ -1,0 +1,112 @@
+// Shared by the host layer and the kernels of the masked attention over a cache (kvs_window_attention and its _packed form).
+#pragma once
+
+#include "kvs_device.h"
+
+namespace kvs {
+
+// One unit of a launch: its rows of the cache.
+struct CacheUnit {
+  long long in_row;
+  int len;
+  int index;            // position in the caller's problem (indexes Q, out, partials)
+};
+
+inline CacheUnit cache_unit(const kvs_problem* p, int i) { return {(long long)p->in_row[i], (int)p->len[i], i}; }
+
+// The units of a launch.  Equal lengths at equal distances (the heads of a layer, or of all layers) follow from the first;
+// up to kInlineUnits others travel in the kernel arguments, more of them through the workspace.  Two types, because a
+// launch with a table in its arguments takes longer (see UnitTableT).
+struct EqualUnits {
+  long long in_row, step;
+  int len, first;
+  __device__ __forceinline__ CacheUnit unit(int i) const { return {in_row + i * step, len, first + i}; }
+};
+struct ListedUnits {
+  const CacheUnit* ext;   // DEVICE, or null: u
+  CacheUnit u[kInlineUnits];
+  __device__ __forceinline__ CacheUnit unit(int i) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+    // (the index is uniform over the workgroup: scalar loads)
+    if (ext != nullptr) return ((const __attribute__((address_space(4))) CacheUnit*)ext)[i];
+#endif
+    return u[i];
+  }
+};
+
+// The cache of a launch.  Plain: k and v are rows of D values.  4 bits: k and v are codes (D / 2 bytes a row), ks and vs the
+// blocks' scales (D / 32 bytes a row).
+struct Cache {
+  const void* k;
+  const void* v;
+  const uint8_t* ks;
+  const uint8_t* vs;
+  const int32_t* counts;
+};
+
+constexpr int kMaxParts = 256;           // pieces that the rows of a unit are cut into at most
+constexpr int kWindowTile = 32;          // cache rows per tile of the kernels in kvs_window_rows.hip
+
+struct WindowShape {
+  int R, G, W, D;
+  int causal;           // 0, or 1: query w is at position len - W + w (0: at len - 1)
+  int span;             // rows up to the query's own that it sees, 0: all
+  int sinks;            // first rows that it sees in any case (and that are not after it)
+  float scale_log2;
+  int block;            // query rows per workgroup
+  int n_blocks;         // per unit
+  int n_parts;          // pieces of the unit and block that has most of them
+  int part_tiles;       // tiles per piece
+};
+
+// Query rows are taken in the order (window position, head), so that a block of them has few positions and its rows of the
+// cache lie together: row r is head r % G at window position r / G.  What a block sees are the rows [0, sink_end) and
+// [first, end), in tiles that start at 0 and at `first`.
+struct Reach {
+  int pos_min, pos_max; // positions of the block's first and last query
+  int sink_end, first, end;
+  int sink_tiles, tiles;
+};
+template <int TILE>
+__host__ __device__ inline Reach reach_of(const WindowShape& sh, int len, int block) {
+  Reach r;
+  const int r0 = block * sh.block;
+  const int r1 = (r0 + sh.block < sh.R ? r0 + sh.block : sh.R) - 1;
+  r.pos_min = sh.causal ? len - sh.W + r0 / sh.G : len - 1;
+  r.pos_max = sh.causal ? len - sh.W + r1 / sh.G : len - 1;
+  r.end = r.pos_max + 1 > 0 ? r.pos_max + 1 : 0;
+  r.first = sh.span > 0 && r.pos_min - sh.span + 1 > 0 ? r.pos_min - sh.span + 1 : 0;
+  if (r.first > r.end) r.first = r.end;
+  r.sink_end = sh.sinks < r.first ? sh.sinks : r.first;
+  r.sink_tiles = (r.sink_end + TILE - 1) / TILE;
+  r.tiles = r.sink_tiles + (r.end - r.first + TILE - 1) / TILE;
+  return r;
+}
+// Whether the query at position `pos` sees row t (0 <= t < the reach's end of t's range).
+__device__ __forceinline__ bool sees(const WindowShape& sh, int pos, int t) {
+  return t <= pos && (sh.span == 0 || t > pos - sh.span || t < sh.sinks);
+}
+// Pieces that a reach of `tiles` tiles is cut into (at least one: it writes the zeros of queries that see nothing).
+__host__ __device__ inline int parts_of(int tiles, int part_tiles) {
+  return tiles <= part_tiles ? 1 : (tiles + part_tiles - 1) / part_tiles;
+}
+
+// Partial results: [unit][query row in the order above][piece] of D numerators, the maximum and the denominator.
+__device__ __forceinline__ size_t part_at(const WindowShape& sh, int unit, int row, int piece) {
+  return (((size_t)unit * sh.R + row) * sh.n_parts + piece) * (size_t)(sh.D + 2);
+}
+// Where query row r of a unit is in Q and out, in rows of D.
+__device__ __forceinline__ size_t query_row(const WindowShape& sh, int unit, int r) {
+  return (size_t)unit * sh.R + (size_t)(r % sh.G) * sh.W + r / sh.G;
+}
+
+enum class CacheKind { kF32, kBf16, kPackedF32, kPackedBf16 };   // the cache, and the type of Q and out
+
+// The launchers: `equal` or, where it is null, `listed`.
+hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
+                              CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
+                              hipStream_t stream);
+// Descriptors of the units from `first` on into the workspace.
+hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, CacheUnit* dst, hipStream_t stream);
+
+}  // namespace kvs

@@ -1,0 +1,296 @@
+// Host layer of the attention with a window and sinks (kvs_window_attention, plain and 4-bit caches) and of the conversions
+// between the two kinds of cache (kvs_pack, kvs_unpack): argument checks, workspace, unit tables, launches.  Everything that
+// can fail because of the arguments fails before the first launch.  Nothing here throws.
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <cstring>
+#include <memory>
+#include <new>
+
+#include "kvs_host.h"
+#include "kvs_pack.h"
+#include "kvs_window.h"
+
+namespace kvs {
+namespace {
+
+constexpr long long kMostRow = 1ll << 48;      // rows that a cache may have: byte offsets stay far below 2^63
+constexpr long long kMostGroups = 1ll << 23;   // workgroups of one launch (a grid has less than 2^32 threads)
+
+// The fields that every one of these calls reads.
+kvs_status check_common(const kvs_problem* p, int* elt) {
+  if (p == nullptr || p->n_units < 1) return KVS_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) return KVS_ERR_INVALID_ARG;
+  int io_dtype;                                // (a caller may have put any integer into the field)
+  std::memcpy(&io_dtype, &p->io_dtype, sizeof(int));
+  if (io_dtype != KVS_F32 && io_dtype != KVS_BF16) return KVS_ERR_DTYPE;
+  if (p->len == nullptr || p->in_row == nullptr) return KVS_ERR_INVALID_ARG;
+  for (int u = 0; u < p->n_units; ++u) {
+    if (p->len[u] < 0 || p->len[u] > KVS_MAX_LEN || p->in_row[u] < 0 || p->in_row[u] > kMostRow) return KVS_ERR_INVALID_ARG;
+  }
+  *elt = io_dtype == KVS_F32 ? 4 : 2;
+  return KVS_OK;
+}
+
+// Rows that the units' ranges reach to.
+size_t rows_to(const kvs_problem* p, const int64_t* first) {
+  long long rows = 0;
+  for (int u = 0; u < p->n_units; ++u) {
+    if (p->len[u] > 0) rows = std::max<long long>(rows, first[u] + p->len[u]);
+  }
+  return (size_t)rows;
+}
+
+kvs_status launched(hipError_t e, const char* what) {
+  if (e == hipSuccess) return KVS_OK;
+  if (debug_switch(KVS_DEBUG_VERBOSE)) std::fprintf(stderr, "libkvs: %s failed: %s\n", what, hipGetErrorString(e));
+  return KVS_ERR_DEVICE;
+}
+
+// ---- attention
+struct WindowPlan {
+  WindowShape sh{};
+  bool equal = false;          // units of one length at equal distances
+  size_t part_bytes = 0, table_bytes = 0;
+  size_t bytes() const { return part_bytes + table_bytes; }
+};
+
+// Most tiles that a block of query rows of a unit of this length reaches (an upper bound of Reach::tiles).
+long long tiles_bound(const WindowShape& sh, int len, int tile) {
+  auto tiles = [&](long long rows) { return (rows + tile - 1) / tile; };
+  if (sh.span == 0) return tiles(len);
+  const long long positions = sh.causal ? std::min<long long>(sh.W, (sh.block - 1) / sh.G + 2) : 1;
+  return tiles(std::min<long long>(len, sh.span + positions - 1)) + tiles(std::min(sh.sinks, len));
+}
+
+// How the rows that a block sees are cut into pieces: workgroups enough for the chip, and pieces long enough for what a
+// workgroup does once.
+void cut_into_parts(const kvs_problem* p, WindowShape& sh) {
+  constexpr long long kWanted = 1024, kLeastTiles = 8;
+  long long total = 0, most = 1;
+  for (int u = 0; u < p->n_units; ++u) {
+    const long long t = tiles_bound(sh, p->len[u], kWindowTile);
+    total += t * sh.n_blocks;
+    most = std::max(most, t);
+  }
+  long long per = std::max((total + kWanted - 1) / kWanted, kLeastTiles);
+  per = std::max(per, (most + kMaxParts - 1) / kMaxParts);
+  sh.part_tiles = (int)per;
+  sh.n_parts = (int)((most + per - 1) / per);
+}
+
+kvs_status make_window_plan(const kvs_problem* p, int32_t span, WindowPlan* plan, int* elt) {
+  const kvs_status st = check_common(p, elt);
+  if (st != KVS_OK) return st;
+  if (p->group < 1 || p->window < 1 || (long long)p->group * p->window > KVS_MAX_WINDOW_ROWS) return KVS_ERR_INVALID_ARG;
+  if (p->n_sink < 0 || span < 0 || (p->causal != 0 && p->causal != 1)) return KVS_ERR_INVALID_ARG;
+  if (!(p->scale >= 0.f) || !std::isfinite(p->scale)) return KVS_ERR_INVALID_ARG;
+  WindowShape& sh = plan->sh;
+  sh.R = p->group * p->window;
+  sh.G = p->group;
+  sh.W = p->window;
+  sh.D = p->head_dim;
+  sh.causal = p->causal;
+  sh.span = std::min(span, KVS_MAX_LEN);       // (a longer one hides nothing, and position - span stays an int)
+  sh.sinks = std::min(p->n_sink, KVS_MAX_LEN);
+  const double scale = p->scale == 0.f ? 1.0 / std::sqrt((double)p->head_dim) : (double)p->scale;
+  sh.scale_log2 = (float)(scale * 1.4426950408889634);
+  sh.block = sh.R <= 16 ? 16 : sh.R <= 32 ? 32 : 64;
+  sh.n_blocks = (sh.R + sh.block - 1) / sh.block;
+  cut_into_parts(p, sh);
+  plan->equal = true;
+  for (int u = 1; u < p->n_units; ++u) {
+    plan->equal = plan->equal && p->len[u] == p->len[0] && p->in_row[u] - p->in_row[u - 1] == p->in_row[1] - p->in_row[0];
+  }
+  if (sh.n_parts > 1) {
+    plan->part_bytes = align_up((size_t)p->n_units * sh.R * sh.n_parts * (sh.D + 2) * sizeof(float));
+  }
+  if (!plan->equal && p->n_units > kInlineUnits) plan->table_bytes = align_up((size_t)p->n_units * sizeof(CacheUnit));
+  return KVS_OK;
+}
+
+struct Buffers {
+  Range r[10];
+  size_t n = 0;
+  void add(const void* p, size_t bytes, bool is_output) {
+    if (bytes > 0) r[n++] = {p, bytes, is_output};           // (a buffer of no rows may be anything)
+  }
+};
+
+kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, const void* Q, const Cache& cache, void* out,
+                            void* ws, size_t ws_bytes, void* hip_stream) {
+  WindowPlan plan;
+  int elt = 0;
+  kvs_status st = make_window_plan(p, span, &plan, &elt);
+  if (st != KVS_OK) return st;
+  const WindowShape& sh = plan.sh;
+  if (plan.bytes() > 0 && (ws == nullptr || ((uintptr_t)ws % kAlign) != 0 || ws_bytes < plan.bytes())) return KVS_ERR_WORKSPACE;
+  const size_t rows = rows_to(p, p->in_row), qo = (size_t)p->n_units * sh.R * sh.D * elt;
+  const size_t row_bytes = packed ? (size_t)sh.D / 2 : (size_t)sh.D * elt;
+  Buffers b;
+  b.add(Q, qo, false);
+  b.add(cache.k, rows * row_bytes, false);
+  b.add(cache.v, rows * row_bytes, false);
+  if (packed) {
+    b.add(cache.ks, rows * (sh.D / 32), false);
+    b.add(cache.vs, rows * (sh.D / 32), false);
+  }
+  if (cache.counts) b.add(cache.counts, rows * 4, false);
+  b.add(out, qo, true);
+  b.add(ws, plan.bytes(), true);
+  if ((st = check_ranges(b.r, b.n)) != KVS_OK) return st;
+
+  const hipStream_t s = (hipStream_t)hip_stream;
+  (void)hipGetLastError();                     // an error left pending by the caller's earlier calls is not this call's
+  float* part = sh.n_parts > 1 ? (float*)ws : nullptr;
+  const CacheUnit* table = nullptr;
+  hipError_t e = hipSuccess;
+  if (plan.table_bytes > 0) {
+    CacheUnit* dst = (CacheUnit*)((char*)ws + plan.part_bytes);
+    table = dst;
+    e = launch_window_table(p, 0, p->n_units, dst, s);
+  }
+  const CacheKind kind = elt == 4 ? (packed ? CacheKind::kPackedF32 : CacheKind::kF32)
+                                  : (packed ? CacheKind::kPackedBf16 : CacheKind::kBf16);
+  // (a call of more workgroups than a grid may have goes out in several launches)
+  const long long groups = std::max<long long>((long long)sh.n_blocks * sh.n_parts, sh.n_parts > 1 ? sh.R : 1);
+  const int most = (int)std::max<long long>(1, kMostGroups / groups);
+  for (int first = 0; e == hipSuccess && first < p->n_units; first += most) {
+    const int n = std::min(most, p->n_units - first);
+    if (plan.equal) {
+      const long long step = p->n_units > 1 ? p->in_row[1] - p->in_row[0] : 0;
+      const EqualUnits units = {p->in_row[first], step, p->len[0], first};
+      e = launch_window_rows(&units, nullptr, n, sh, kind, cache, Q, out, part, s);
+    } else {
+      ListedUnits units;
+      units.ext = table ? table + first : nullptr;
+      for (int i = 0; i < kInlineUnits; ++i) units.u[i] = cache_unit(p, first + std::min(i, n - 1));
+      e = launch_window_rows(nullptr, &units, n, sh, kind, cache, Q, out, part, s);
+    }
+  }
+  return launched(e, "an attention launch");
+}
+
+// ---- conversions
+// The units' destination ranges are disjoint.
+kvs_status check_disjoint(const kvs_problem* p) {
+  auto end = [&](int u) { return (long long)p->out_row[u] + p->len[u]; };
+  bool ascending = true;
+  for (int u = 1; u < p->n_units; ++u) ascending = ascending && end(u - 1) <= p->out_row[u];
+  if (ascending) return KVS_OK;
+  std::unique_ptr<int[]> order(new (std::nothrow) int[p->n_units]);
+  if (!order) return KVS_ERR_DEVICE;
+  int n = 0;
+  for (int u = 0; u < p->n_units; ++u) {
+    if (p->len[u] > 0) order[n++] = u;
+  }
+  std::sort(order.get(), order.get() + n, [&](int a, int b) { return p->out_row[a] < p->out_row[b]; });
+  for (int i = 1; i < n; ++i) {
+    if (end(order[i - 1]) > p->out_row[order[i]]) return KVS_ERR_INVALID_ARG;
+  }
+  return KVS_OK;
+}
+
+// The checks of both directions, then f(equal, listed, n_units, longest) for every launch.  rows, packed: K, V and the four
+// packed arrays; to_packed: which side is written.
+template <typename F>
+kvs_status convert(const kvs_problem* p, const void* K, const void* V, const PackedRange& c, bool to_packed, F&& f) {
+  int elt = 0;
+  kvs_status st = check_common(p, &elt);
+  if (st != KVS_OK) return st;
+  if (p->out_row == nullptr) return KVS_ERR_INVALID_ARG;
+  for (int u = 0; u < p->n_units; ++u) {
+    if (p->out_row[u] < 0 || p->out_row[u] > kMostRow) return KVS_ERR_INVALID_ARG;
+  }
+  if ((st = check_disjoint(p)) != KVS_OK) return st;
+  const size_t plain = rows_to(p, to_packed ? p->in_row : p->out_row), coded = rows_to(p, to_packed ? p->out_row : p->in_row);
+  const size_t D = (size_t)p->head_dim;
+  Buffers b;
+  b.add(K, plain * D * elt, !to_packed);
+  b.add(V, plain * D * elt, !to_packed);
+  b.add(c.kc, coded * (D / 2), to_packed);
+  b.add(c.ks, coded * (D / 32), to_packed);
+  b.add(c.vc, coded * (D / 2), to_packed);
+  b.add(c.vs, coded * (D / 32), to_packed);
+  if ((st = check_ranges(b.r, b.n)) != KVS_OK) return st;
+
+  (void)hipGetLastError();
+  auto move = [&](int u) { return RowMove{p->in_row[u], p->out_row[u], p->len[u]}; };
+  hipError_t e = hipSuccess;
+  for (int first = 0, n = 0; e == hipSuccess && first < p->n_units; first += n) {
+    EqualMoves equal = {move(first), 0, 0};
+    n = 1;
+    if (first + 1 < p->n_units) {
+      equal.src_step = p->in_row[first + 1] - p->in_row[first];
+      equal.dst_step = p->out_row[first + 1] - p->out_row[first];
+    }
+    while (n < kMostMoves && first + n < p->n_units && p->len[first + n] == p->len[first] &&
+           p->in_row[first + n] - p->in_row[first + n - 1] == equal.src_step &&
+           p->out_row[first + n] - p->out_row[first + n - 1] == equal.dst_step) {
+      ++n;
+    }
+    const int listed_n = std::min(kListedMoves, p->n_units - first);
+    if (n >= listed_n) {                       // the longer run of the two
+      if (equal.first.len > 0) e = f(&equal, (const ListedMoves*)nullptr, n, equal.first.len);
+      continue;
+    }
+    n = listed_n;
+    ListedMoves listed;
+    int longest = 0;
+    for (int i = 0; i < kListedMoves; ++i) {
+      listed.u[i] = move(first + std::min(i, n - 1));
+      longest = std::max(longest, listed.u[i].len);
+    }
+    if (longest > 0) e = f((const EqualMoves*)nullptr, &listed, n, longest);
+  }
+  return launched(e, "a conversion launch");
+}
+
+}  // namespace
+}  // namespace kvs
+
+using namespace kvs;
+
+extern "C" {
+
+kvs_status kvs_window_attention_workspace_size(const kvs_problem* p, int32_t span, size_t* bytes) {
+  if (bytes == nullptr) return KVS_ERR_INVALID_ARG;
+  WindowPlan plan;
+  int elt = 0;
+  const kvs_status st = make_window_plan(p, span, &plan, &elt);
+  if (st != KVS_OK) return st;
+  *bytes = plan.bytes();
+  return KVS_OK;
+}
+
+kvs_status kvs_window_attention(const kvs_problem* p, int32_t span, const void* Q, const void* K, const void* V,
+                                const int32_t* counts, void* out, void* ws, size_t ws_bytes, void* hip_stream) {
+  const Cache cache = {K, V, nullptr, nullptr, counts};
+  return window_attention(p, span, /*packed=*/false, Q, cache, out, ws, ws_bytes, hip_stream);
+}
+
+kvs_status kvs_window_attention_packed(const kvs_problem* p, int32_t span, const void* Q, const void* K_codes,
+                                       const void* K_scales, const void* V_codes, const void* V_scales,
+                                       const int32_t* counts, void* out, void* ws, size_t ws_bytes, void* hip_stream) {
+  const Cache cache = {K_codes, V_codes, (const uint8_t*)K_scales, (const uint8_t*)V_scales, counts};
+  return window_attention(p, span, /*packed=*/true, Q, cache, out, ws, ws_bytes, hip_stream);
+}
+
+kvs_status kvs_pack(const kvs_problem* p, const void* K, const void* V, void* K_codes, void* K_scales, void* V_codes,
+                    void* V_scales, void* hip_stream) {
+  const PackedRange to = {(uint8_t*)K_codes, (uint8_t*)K_scales, (uint8_t*)V_codes, (uint8_t*)V_scales};
+  return convert(p, K, V, to, /*to_packed=*/true, [&](const EqualMoves* equal, const ListedMoves* listed, int n, int longest) {
+    return launch_pack(equal, listed, n, longest, p->io_dtype, p->head_dim, K, V, to, (hipStream_t)hip_stream);
+  });
+}
+
+kvs_status kvs_unpack(const kvs_problem* p, const void* K_codes, const void* K_scales, const void* V_codes,
+                      const void* V_scales, void* K, void* V, void* hip_stream) {
+  const PackedRange from = {(uint8_t*)K_codes, (uint8_t*)K_scales, (uint8_t*)V_codes, (uint8_t*)V_scales};
+  return convert(p, K, V, from, /*to_packed=*/false, [&](const EqualMoves* equal, const ListedMoves* listed, int n, int longest) {
+    return launch_unpack(equal, listed, n, longest, p->io_dtype, p->head_dim, from, K, V, (hipStream_t)hip_stream);
+  });
+}
+
+}  // extern "C"

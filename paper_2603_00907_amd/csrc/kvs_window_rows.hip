@@ -1,0 +1,594 @@
+// Attention of a unit's query rows over its cache under a causal mask, a sliding window and first rows that stay visible:
+//   out[q] = sum_t exp(e_t) V[t] / sum_t c_t exp(e_t),   e_t = scale * q . k_t,   over the rows t that q sees
+// (sees()); a query that sees none gets zeros.  The cache is plain rows (fp32, bf16) or rows in 4 bits.
+//
+// A workgroup takes a block of 16 NQ query rows of one unit and a piece of the rows that they see; its wavefronts take the
+// piece's tiles of 32 rows in turn, each with a softmax of its own (running maximum, denominator and numerators), and
+// never wait for each other until the piece is done.  Both products are on the matrix cores, 16 query rows per column
+// block (a decode step of one token has 4 to 8, so that 16 waste the least), and nothing passes through LDS:
+//   S = K Q^T       the lane's row of K as it lies in memory (the contraction index, a channel, may be split between the
+//                   lane groups in any way that both operands share);
+//   O^T += V^T P    a lane holds D / 16 neighbouring channels of the eight rows that are its share of the contraction:
+//                   those whose logits the first product has left in the same lane group, so that P is already in
+//                   operand order.  bf16 pairs of neighbouring channels become pairs of neighbouring rows by byte moves.
+// 4-bit rows are turned into bf16 in registers (exact: four significant bits times a power of two), two values per
+// instruction, and fp32 rows go through the fp32 matrix instructions.
+//
+// A product with P = 0 is not nothing where V is not finite, so in a tile that some query of the block does not see whole
+// such values are left out of the product; when the piece is done they are added for the queries that see their row.
+#include <type_traits>
+
+#include "kvs_fp4.h"
+#include "kvs_window.h"
+
+namespace kvs {
+namespace {
+
+using fp4::scale_of;
+using fp4::two_of;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kTile = kWindowTile;
+// The running maximum is raised only when a logit exceeds it by this many powers of two: terms up to 2^8 are as exact.
+constexpr float kSlack = 8.f;
+
+// A piece of a unit's rows (at most 2^31 bytes of them): one scalar base, 32-bit offsets.
+template <typename T>
+__device__ __forceinline__ T at(const char* base, uint32_t offset) { return *(const T*)(base + offset); }
+
+// x as a sum of N bf16 numbers, each the rounding of what the ones before leave (N = 3: exact but for the last bits of
+// fp32, 2^-24 of x; N = 2: 2^-17).  An infinity or NaN stays one in the first.
+template <int N>
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&s)[N]) {
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = cvt_pk_bf16(r[2 * i], r[2 * i + 1]);
+    s[n] = __builtin_bit_cast(bf16x8, w);
+    if (n + 1 < N) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float lo = bf16_lo(w[i]), hi = bf16_hi(w[i]);
+        // (what is left of an infinity would be a NaN)
+        r[2 * i] = __builtin_isfinite(lo) ? r[2 * i] - lo : 0.f;
+        r[2 * i + 1] = __builtin_isfinite(hi) ? r[2 * i + 1] - hi : 0.f;
+      }
+    }
+  }
+}
+
+// What a wavefront reads of a tile of 32 rows.  Lane l of the wavefront is column / row c = l % 16 of lane group g = l / 16;
+// key rows: 16 h + c (h = 0, 1), value rows: i < 4: 4 g + i, else 12 + 4 g + i.
+template <CacheKind KIND, int D> struct Rows;
+
+template <int D>
+struct Rows<CacheKind::kBf16, D> {
+  typedef uint16_t Io;
+  static constexpr bool kMatrixF32 = false;
+  static constexpr int kQ = 1, kP = 2;     // bf16 numbers that a query value and a weight are taken as
+  static constexpr int kSteps = D / 32;
+  static constexpr int CPL = D / 16;       // channels of a value row per lane
+  typedef uint32_t vpiece __attribute__((ext_vector_type(CPL / 2)));
+  u32x4 k[2][kSteps];
+  vpiece v[8];
+  static __device__ __forceinline__ int channel(int s, int g) { return 32 * s + 8 * g; }
+  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int h, uint32_t row, int g) {
+    const char* base = (const char*)cache.k + row0 * (2 * D);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) k[h][s] = at<u32x4>(base, row * (2 * D) + 16 * g + 64 * s);
+  }
+  __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
+    v[i] = at<vpiece>((const char*)cache.v + row0 * (2 * D), row * (2 * D) + c * (D / 8));
+  }
+  static __device__ __forceinline__ f32x4 four_values(const Cache& cache, size_t row0, uint32_t row, int ch) {
+    const uint2 x = at<uint2>((const char*)cache.v + row0 * (2 * D), row * (2 * D) + 2 * ch);
+    return f32x4{bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y)};
+  }
+  __device__ __forceinline__ bf16x8 key(int h, int s) const { return __builtin_bit_cast(bf16x8, k[h][s]); }
+  // channels 2 W, 2 W + 1 of the lane's
+  template <int W> __device__ __forceinline__ uint32_t value(int i) const { return v[i][W]; }
+};
+
+template <int D, bool F32>
+struct PackedRows {
+  typedef std::conditional_t<F32, float, uint16_t> Io;
+  static constexpr bool kMatrixF32 = false;
+  static constexpr int kQ = F32 ? 3 : 1, kP = F32 ? 3 : 2;
+  static constexpr int kSteps = D / 32;
+  static constexpr int CPL = D / 16;
+  typedef uint32_t kpiece __attribute__((ext_vector_type(D / 32)));
+  typedef std::conditional_t<D == 128, uint32_t, uint16_t> vpiece;
+  kpiece k[2];
+  uint8_t ks[2];
+  vpiece v[8];
+  uint8_t vs[8];
+  static __device__ __forceinline__ int channel(int s, int g) { return (D / 4) * g + 8 * s; }
+  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int h, uint32_t row, int g) {
+    k[h] = at<kpiece>((const char*)cache.k + row0 * (D / 2), row * (D / 2) + g * (D / 8));
+    ks[h] = at<uint8_t>((const char*)cache.ks + row0 * (D / 32), row * (D / 32) + g * (D / 4) / 32);
+  }
+  __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
+    v[i] = at<vpiece>((const char*)cache.v + row0 * (D / 2), row * (D / 2) + c * (D / 32));
+    vs[i] = at<uint8_t>((const char*)cache.vs + row0 * (D / 32), row * (D / 32) + c * CPL / 32);
+  }
+  static __device__ __forceinline__ f32x4 four_values(const Cache& cache, size_t row0, uint32_t row, int ch) {
+    const uint32_t x = at<uint16_t>((const char*)cache.v + row0 * (D / 2), row * (D / 2) + ch / 2);
+    const float sc = scale_of(at<uint8_t>((const char*)cache.vs + row0 * (D / 32), row * (D / 32) + ch / 32));
+    const uint32_t a = two_of<0>(x, sc), b = two_of<1>(x, sc);
+    return f32x4{bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)};
+  }
+  __device__ __forceinline__ bf16x8 key(int h, int s) const {
+    const float sc = scale_of(ks[h]);
+    const u32x4 w = {two_of<0>(k[h][s], sc), two_of<1>(k[h][s], sc), two_of<2>(k[h][s], sc), two_of<3>(k[h][s], sc)};
+    return __builtin_bit_cast(bf16x8, w);
+  }
+  template <int W> __device__ __forceinline__ uint32_t value(int i) const { return two_of<W>(v[i], scale_of(vs[i])); }
+};
+template <int D> struct Rows<CacheKind::kPackedBf16, D> : PackedRows<D, false> {};
+template <int D> struct Rows<CacheKind::kPackedF32, D> : PackedRows<D, true> {};
+
+template <int D>
+struct Rows<CacheKind::kF32, D> {
+  typedef float Io;
+  static constexpr bool kMatrixF32 = true;
+  static constexpr int kQ = 1, kP = 1;
+  static constexpr int kSteps = D / 16;
+  f32x4 k[2][kSteps];
+  f32x4 v[8][D / 64];
+  static __device__ __forceinline__ int channel(int s, int g) { return 16 * s + 4 * g; }
+  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int h, uint32_t row, int g) {
+    const char* base = (const char*)cache.k + row0 * (4 * D);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) k[h][s] = at<f32x4>(base, row * (4 * D) + 16 * g + 64 * s);
+  }
+  __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
+    const char* base = (const char*)cache.v + row0 * (4 * D);
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) v[i][e] = at<f32x4>(base, row * (4 * D) + 16 * c + 256 * e);
+  }
+  static __device__ __forceinline__ f32x4 four_values(const Cache& cache, size_t row0, uint32_t row, int ch) {
+    return at<f32x4>((const char*)cache.v + row0 * (4 * D), row * (4 * D) + 4 * ch);
+  }
+};
+
+// The block's query rows as the second operand of S = K Q^T.
+template <typename L, int D, int NQ>
+struct Queries {
+  std::conditional_t<L::kMatrixF32, f32x4, bf16x8> q[NQ][L::kQ][L::kSteps];
+  __device__ __forceinline__ void load(const typename L::Io* Q, const WindowShape& sh, int unit, int row0, int c, int g) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const int r = min(row0 + 16 * n + c, sh.R - 1);        // rows past R repeat the last one
+      const typename L::Io* src = Q + query_row(sh, unit, r) * D;
+#pragma unroll
+      for (int s = 0; s < L::kSteps; ++s) {
+        const typename L::Io* at = src + L::channel(s, g);
+        if constexpr (L::kMatrixF32) {
+          q[n][0][s] = *(const f32x4*)at;
+        } else if constexpr (std::is_same_v<typename L::Io, float>) {
+          float x[8];
+          *(f32x4*)&x[0] = *(const f32x4*)at;
+          *(f32x4*)&x[4] = *((const f32x4*)at + 1);
+          bf16x8 part[L::kQ];
+          split8<L::kQ>(x, part);
+#pragma unroll
+          for (int k = 0; k < L::kQ; ++k) q[n][k][s] = part[k];
+        } else {
+          q[n][0][s] = *(const bf16x8*)at;
+        }
+      }
+    }
+  }
+};
+
+// First of the four neighbouring channels that accumulators 4 j4 .. 4 j4 + 3 of O^T hold in accumulator row r.
+template <bool F32, int D>
+__device__ __forceinline__ int channel_of(int j4, int r) {
+  return F32 ? 64 * j4 + 4 * r : (D / 16) * r + 4 * j4;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_two(T* at, float a, float b) {
+  if constexpr (std::is_same_v<T, float>) *(float2*)at = make_float2(a, b);
+  else *(uint32_t*)at = cvt_pk_bf16(a, b);
+}
+// A numerator over its denominator; zero where no term was seen.
+__device__ __forceinline__ float quotient(float num, float den) { return den == 0.f ? 0.f : num / den; }
+
+template <CacheKind KIND, int D, int NQ, typename Tab>
+__global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void window_rows_kernel(
+    const Tab tab, const WindowShape sh, const Cache cache, const void* __restrict__ Q, void* __restrict__ out,
+    float* __restrict__ part) {
+  typedef Rows<KIND, D> L;
+  typedef typename L::Io Io;
+  constexpr bool F32 = L::kMatrixF32;
+  constexpr int NJ = D / 16;                // accumulators of O^T per column block
+  constexpr int ACCW = D + 4;               // numerators, maximum, denominator; rows stay 16-byte aligned
+  __shared__ __attribute__((aligned(16))) float sm_acc[kWaves][16][ACCW];
+
+  const int id = blockIdx.x;
+  const int piece = id % sh.n_parts, block = id / sh.n_parts % sh.n_blocks;
+  const CacheUnit un = tab.unit(id / sh.n_parts / sh.n_blocks);
+  const Reach re = reach_of<kTile>(sh, un.len, block);
+  const int n_parts = parts_of(re.tiles, sh.part_tiles);
+  if (piece >= n_parts) return;             // the grid is as wide as the longest reach needs
+  const int tile1 = min(re.tiles, (piece + 1) * sh.part_tiles);
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  const int c = lane % 16, g = lane / 16;
+  const int row0 = block * sh.block;
+
+  int pos[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    pos[n] = sh.causal ? un.len - sh.W + min(row0 + 16 * n + c, sh.R - 1) / sh.G : un.len - 1;
+  }
+  f32x4 acc[NQ][NJ];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m[n] = -INFINITY;
+    l[n] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  int j = piece * sh.part_tiles + wave;
+  if (j < tile1) {
+    Queries<L, D, NQ> qs;
+    qs.load((const Io*)Q, sh, un.index, row0, c, g);
+    L rows;
+    float cnt[8];
+    // tile j: its first row, and the end of the range of rows that it is in (rows past it repeat the last one)
+    auto start_of = [&](int t) { return t < re.sink_tiles ? t * kTile : re.first + (t - re.sink_tiles) * kTile; };
+    auto end_of = [&](int t) { return t < re.sink_tiles ? re.sink_end : re.end; };
+    // every row of the tile is seen by the whole block
+    auto seen_whole = [&](int t0, int end) {
+      return t0 + kTile <= end && t0 + kTile - 1 <= re.pos_min &&
+             (sh.span == 0 || t0 > re.pos_max - sh.span || t0 + kTile <= sh.sinks);
+    };
+    auto load_keys = [&](int t) {
+      const int t0 = start_of(t), last = end_of(t) - 1;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) rows.load_keys(cache, un.in_row, h, min(t0 + 16 * h + c, last), g);
+    };
+    auto load_values = [&](int t) {
+      const int t0 = start_of(t), last = end_of(t) - 1;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = min(t0 + (i < 4 ? 0 : 12) + 4 * g + i, last);
+        rows.load_value(cache, un.in_row, i, row, c);
+        cnt[i] = cache.counts ? (float)cache.counts[un.in_row + row] : 1.f;
+      }
+    };
+    const int j0 = j;
+    bool odd = false;                       // a value that is not finite was left out
+    load_keys(j);
+    load_values(j);
+    while (true) {
+      const int t0 = start_of(j), end = end_of(j);
+      const int next = j + kWaves;
+      // S[t, q]: element v of half h is row 16 h + 4 g + v of the tile, query column c
+      f32x4 s[NQ][2];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int st = 0; st < L::kSteps; ++st) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+#pragma unroll
+              for (int n = 0; n < NQ; ++n)
+                s[n][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(rows.k[h][st][e], qs.q[n][0][st][e], s[n][h], 0, 0, 0);
+            }
+          } else {
+            const bf16x8 a = rows.key(h, st);
+#pragma unroll
+            for (int k = L::kQ - 1; k >= 0; --k) {           // (the small parts first)
+#pragma unroll
+              for (int n = 0; n < NQ; ++n)
+                s[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qs.q[n][k][st], s[n][h], 0, 0, 0);
+            }
+          }
+        }
+      }
+      if (next < tile1) load_keys(next);
+      const bool whole = seen_whole(t0, end);
+      float p[NQ][8];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int t = t0 + (i < 4 ? 0 : 12) + 4 * g + i;
+          const float x = s[n][i / 4][i % 4] * sh.scale_log2;
+          p[n][i] = whole || (t < end && sees(sh, pos[n], t)) ? x : -INFINITY;
+          top = fmaxf(top, p[n][i]);
+        }
+        if (__ballot(top > m[n] + kSlack) != 0) {            // rare after the first tiles
+          top = fmaxf(top, __shfl_xor(top, 16, kWave));      // the four lane groups feed the same columns of O^T
+          top = fmaxf(top, __shfl_xor(top, 32, kWave));
+          top = fmaxf(top, m[n]);
+          const float corr = m[n] == top ? 1.f : __builtin_amdgcn_exp2f(m[n] - top);
+          l[n] *= corr;
+#pragma unroll
+          for (int k = 0; k < NJ; ++k) acc[n][k] *= corr;
+          m[n] = top;
+        }
+        const float ref = m[n] == -INFINITY ? 0.f : m[n];    // (a query that has seen nothing yet)
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[n][i] = __builtin_amdgcn_exp2f(p[n][i] - ref);
+          sum = fmaf(cnt[i], p[n][i], sum);                  // c copies of the slot in the denominator
+        }
+        l[n] += sum;
+      }
+      // V^T: of bf16 pairs of channels become pairs of rows, operand k is channel k of the lane's, element i the lane's row i
+      u32x4 vt[F32 ? 1 : NJ];
+      if constexpr (!F32) {
+        auto turn = [&](auto w) {
+          constexpr int W2 = decltype(w)::value;
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const uint32_t a = rows.template value<W2>(i), b = rows.template value<W2>(i + 1);
+            vt[2 * W2][i / 2] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+            vt[2 * W2 + 1][i / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+          }
+        };
+        turn(std::integral_constant<int, 0>{});
+        turn(std::integral_constant<int, 1>{});
+        if constexpr (NJ == 8) {
+          turn(std::integral_constant<int, 2>{});
+          turn(std::integral_constant<int, 3>{});
+        }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int k = 0; k < NJ; ++k) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float x = rows.v[i][k / 4][k % 4];
+              const bool bad = !__builtin_isfinite(x);
+              odd |= bad;
+              rows.v[i][k / 4][k % 4] = bad ? 0.f : x;
+            }
+          } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t x = vt[k][w];
+              const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
+              odd |= lo | hi;
+              vt[k][w] = x & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+            }
+          }
+        }
+      }
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+          for (int k = 0; k < NJ; ++k) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+              acc[n][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(rows.v[i][k / 4][k % 4], p[n][i], acc[n][k], 0, 0, 0);
+          }
+        }
+      } else {
+        bf16x8 pp[NQ][L::kP];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) split8<L::kP>(p[n], pp[n]);
+#pragma unroll
+        for (int k = 0; k < NJ; ++k) {
+#pragma unroll
+          for (int h = L::kP - 1; h >= 0; --h) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+              acc[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt[k]), pp[n][h], acc[n][k], 0, 0, 0);
+          }
+        }
+      }
+      if (next >= tile1) break;
+      load_values(next);
+      j = next;
+    }
+    if (__ballot(odd) != 0) {
+      // What is not finite makes the sums of the queries that see it what it is itself, whatever its weight.
+      for (j = j0; j < tile1; j += kWaves) {
+        const int t0 = start_of(j), end = end_of(j);
+        if (seen_whole(t0, end)) continue;
+#pragma unroll 1
+        for (int t = t0; t < min(t0 + kTile, end); ++t) {
+#pragma unroll
+          for (int j4 = 0; j4 < NJ / 4; ++j4) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const f32x4 y = L::four_values(cache, un.in_row, t, channel_of<F32, D>(j4, 4 * g + v));
+#pragma unroll
+              for (int n = 0; n < NQ; ++n) {
+                const bool seen = sees(sh, pos[n], t);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[n][4 * j4 + e][v] += seen && !__builtin_isfinite(y[e]) ? y[e] : 0.f;
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // the wavefronts of the workgroup, in wavefront order
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    float den = l[n] + __shfl_xor(l[n], 16, kWave);
+    den += __shfl_xor(den, 32, kWave);
+    if (n > 0) __syncthreads();
+#pragma unroll
+    for (int j4 = 0; j4 < NJ / 4; ++j4) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        *(float4*)&sm_acc[wave][c][channel_of<F32, D>(j4, 4 * g + v)] =
+            make_float4(acc[n][4 * j4][v], acc[n][4 * j4 + 1][v], acc[n][4 * j4 + 2][v], acc[n][4 * j4 + 3][v]);
+      }
+    }
+    if (g == 0) { sm_acc[wave][c][D] = m[n]; sm_acc[wave][c][D + 1] = den; }
+    __syncthreads();
+    for (int o = tid; o < 16 * D / 2; o += kThreads) {
+      const int q = o / (D / 2), ch = o % (D / 2) * 2, row = row0 + 16 * n + q;
+      if (row >= min(sh.R, row0 + sh.block)) continue;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_acc[w][q][D]);
+      float a = 0.f, b = 0.f, den_q = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float lw = sm_acc[w][q][D + 1];
+        if (lw != 0.f) {                                     // (a wavefront that saw no row has m = -inf)
+          const float wgt = __builtin_amdgcn_exp2f(sm_acc[w][q][D] - M);
+          a = fmaf(sm_acc[w][q][ch], wgt, a);
+          b = fmaf(sm_acc[w][q][ch + 1], wgt, b);
+          den_q = fmaf(lw, wgt, den_q);
+        }
+      }
+      if (sh.n_parts == 1) {
+        store_two((Io*)out + query_row(sh, un.index, row) * D + ch, quotient(a, den_q), quotient(b, den_q));
+      } else {
+        float* dst = part + part_at(sh, un.index, row, piece);
+        *(float2*)(dst + ch) = make_float2(a, b);
+        if (ch == 0) { dst[D] = M; dst[D + 1] = den_q; }
+      }
+    }
+  }
+}
+
+// out[row] from its pieces, in order.  One workgroup per (unit, query row): thread (g, d) adds up every PARTS-th piece of
+// channel d, and the sums are added in order.
+template <typename Io, int D, int TILE, typename Tab>
+__global__ __launch_bounds__(kThreads) void window_reduce_kernel(const Tab tab, const WindowShape sh,
+                                                                 const float* __restrict__ part, void* __restrict__ out) {
+  constexpr int PARTS = kThreads / D;
+  __shared__ float sm_w[kMaxParts];
+  __shared__ float sm_num[PARTS][D];
+  __shared__ float sm_top[kWaves], sm_den[kWaves];
+  const CacheUnit un = tab.unit(blockIdx.x / sh.R);
+  const int row = blockIdx.x % sh.R;
+  const int n = parts_of(reach_of<TILE>(sh, un.len, row / sh.block).tiles, sh.part_tiles);
+  const float* src = part + part_at(sh, un.index, row, 0);
+  const int tid = threadIdx.x, d = tid % D, g = tid / D;
+  const float m = tid < n ? src[(size_t)tid * (D + 2) + D] : -INFINITY;
+  const float l = tid < n ? src[(size_t)tid * (D + 2) + D + 1] : 0.f;
+  float M = m;
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor(M, k, kWave));
+  if (tid % kWave == 0) sm_top[tid / kWave] = M;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_top[w]);
+  const float wgt = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M);
+  if (tid < n) sm_w[tid] = wgt;
+  float den = l == 0.f ? 0.f : l * wgt;
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) den += __shfl_xor(den, k, kWave);
+  if (tid % kWave == 0) sm_den[tid / kWave] = den;
+  __syncthreads();
+  float num = 0.f;
+  for (int i0 = g; i0 < n; i0 += 8 * PARTS) {                // eight loads at a time
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = src[(size_t)min(i0 + u * PARTS, n - 1) * (D + 2) + d];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (i0 + u * PARTS < n) num = fmaf(x[u], sm_w[i0 + u * PARTS], num);
+    }
+  }
+  sm_num[g][d] = num;
+  __syncthreads();
+  if (tid < D / 2) {
+    float a = 0.f, b = 0.f, total = 0.f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) { a += sm_num[i][2 * tid]; b += sm_num[i][2 * tid + 1]; }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total += sm_den[w];
+    store_two((Io*)out + query_row(sh, un.index, row) * D + 2 * tid, quotient(a, total), quotient(b, total));
+  }
+}
+
+// Unit descriptors of a launch that has too many for its arguments, stored by a kernel that carries some in its own.
+constexpr int kTableBatch = 224;
+struct CacheUnitBatch { CacheUnit u[kTableBatch]; };
+__global__ __launch_bounds__(256) void cache_unit_table_kernel(const CacheUnitBatch batch, int n, CacheUnit* __restrict__ dst) {
+  const int i = threadIdx.x;
+  if (i < n) dst[i] = batch.u[i];
+}
+
+template <CacheKind KIND, int D, typename Tab>
+hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
+                       float* part, hipStream_t stream) {
+  typedef typename Rows<KIND, D>::Io Io;
+  const dim3 grid((unsigned)((long long)n_units * sh.n_blocks * sh.n_parts));
+  auto go = [&](auto nq) {
+    hipLaunchKernelGGL((window_rows_kernel<KIND, D, decltype(nq)::value, Tab>), grid, dim3(kThreads), 0, stream, tab, sh,
+                       cache, Q, out, part);
+  };
+  if (sh.block == 16) go(std::integral_constant<int, 1>{});
+  else if (sh.block == 32) go(std::integral_constant<int, 2>{});
+  else go(std::integral_constant<int, 4>{});
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sh.n_parts == 1) return e;
+  hipLaunchKernelGGL((window_reduce_kernel<Io, D, kTile, Tab>), dim3((unsigned)((long long)n_units * sh.R)), dim3(kThreads),
+                     0, stream, tab, sh, part, out);
+  return hipGetLastError();
+}
+
+template <CacheKind KIND, typename Tab>
+hipError_t launch_d(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
+                    float* part, hipStream_t stream) {
+  return sh.D == 64 ? launch_kind<KIND, 64>(tab, n_units, sh, cache, Q, out, part, stream)
+                    : launch_kind<KIND, 128>(tab, n_units, sh, cache, Q, out, part, stream);
+}
+
+template <typename Tab>
+hipError_t launch_tab(const Tab& tab, int n_units, const WindowShape& sh, CacheKind kind, const Cache& cache,
+                      const void* Q, void* out, float* part, hipStream_t stream) {
+  switch (kind) {
+    case CacheKind::kF32: return launch_d<CacheKind::kF32>(tab, n_units, sh, cache, Q, out, part, stream);
+    case CacheKind::kBf16: return launch_d<CacheKind::kBf16>(tab, n_units, sh, cache, Q, out, part, stream);
+    case CacheKind::kPackedF32: return launch_d<CacheKind::kPackedF32>(tab, n_units, sh, cache, Q, out, part, stream);
+    default: return launch_d<CacheKind::kPackedBf16>(tab, n_units, sh, cache, Q, out, part, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
+                              CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
+                              hipStream_t stream) {
+  if (equal) return launch_tab(*equal, n_units, sh, kind, cache, Q, out, part, stream);
+  return launch_tab(*listed, n_units, sh, kind, cache, Q, out, part, stream);
+}
+
+hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, CacheUnit* dst, hipStream_t stream) {
+  for (int at = 0; at < n_units; at += kTableBatch) {
+    const int n = n_units - at < kTableBatch ? n_units - at : kTableBatch;
+    CacheUnitBatch batch;
+    for (int i = 0; i < kTableBatch; ++i) batch.u[i] = cache_unit(p, first + at + (i < n ? i : 0));
+    hipLaunchKernelGGL(cache_unit_table_kernel, dim3(1), dim3(256), 0, stream, batch, n, dst + at);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace kvs

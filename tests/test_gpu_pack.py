@@ -1,0 +1,143 @@
+"""kvs_pack and kvs_unpack: codes, scales and values bit for bit against the definition."""
+
+import numpy as np
+import pytest
+
+import window_reference as R
+from helpers import from_device, to_device, torch_io_dtype
+
+pytestmark = pytest.mark.gpu
+
+KINDS = [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)]
+
+
+def packed_buffers(rows, D, fill=0xA5):
+    import torch
+    return [torch.full((rows, D // per), fill, dtype=torch.uint8, device="cuda") for per in (2, 32, 2, 32)]
+
+
+def pack_all(K, V, dtype, D):
+    """One unit of all rows, through the library."""
+    import torch
+    import paper_2603_00907_amd as kvs
+    n = K.shape[0]
+    p = kvs.Problem(lens=[n], budgets=[n], group=1, window=1, head_dim=D, dtype=dtype)
+    buf = packed_buffers(n, D)
+    kvs.kvs_pack(p, to_device(K, dtype), to_device(V, dtype), *buf, stream=torch.cuda.current_stream().cuda_stream)
+    back = [torch.empty(n, D, dtype=torch_io_dtype(dtype), device="cuda") for _ in range(2)]
+    kvs.kvs_unpack(p, *buf, *back, stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return [b.cpu().numpy() for b in buf], [from_device(b) for b in back]
+
+
+def check(K, V, dtype, D):
+    (kc, ks, vc, vs), back = pack_all(K, V, dtype, D)
+    for x, codes, scales, values in ((K, kc, ks, back[0]), (V, vc, vs, back[1])):
+        want_codes, want_scales = R.pack(x)
+        assert (scales == want_scales).all()
+        assert (codes == want_codes).all()
+        want = R.unpack(want_codes, want_scales)
+        assert (np.isnan(values) == np.isnan(want)).all()
+        assert (values[~np.isnan(want)] == want[~np.isnan(want)]).all()
+
+
+def rows_of(rng, n, D, dtype):
+    x = (rng.standard_normal((n, D)) * np.exp2(rng.integers(-20, 20, (n, 1)))).astype(np.float32)
+    x[rng.random((n, D)) < 0.05] = 0
+    return R.bf16(x) if dtype == "bf16" else x
+
+
+@pytest.mark.parametrize("dtype,D", KINDS)
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 63, 64, 65, 129, 1000])
+def test_rows_of_every_kind(dtype, D, n):
+    rng = np.random.default_rng(n)
+    check(rows_of(rng, n, D, dtype), rows_of(rng, n, D, dtype), dtype, D)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_all_bf16_numbers(D):
+    """Every bit pattern, beside numbers of its own size, once in order and once beside others."""
+    bits = np.arange(65536, dtype=np.uint32)
+    x = (bits << 16).view(np.float32)
+    rng = np.random.default_rng(3)
+    finite = x[np.isfinite(x)]
+    rest = rng.permutation(finite)
+    check(x.reshape(-1, D), np.concatenate([rest, rest[:65536 - len(rest)]]).reshape(-1, D), "bf16", D)
+
+
+def test_ties_and_the_ends_of_the_range_in_fp32():
+    rng = np.random.default_rng(4)
+    middles = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 6.0], dtype=np.float32)
+    near = np.concatenate([middles, np.nextafter(middles, np.float32(0)), np.nextafter(middles, np.float32(9))])
+    rows = []
+    for e in list(range(-149, 126, 7)) + [-126, -125, -124, 124, 125]:
+        row = rng.choice(np.concatenate([near, -near]), 128).astype(np.float64) * 2.0 ** e
+        rows.append(np.clip(row, -np.finfo(np.float32).max, np.finfo(np.float32).max))
+    x = np.array(rows).astype(np.float32)
+    big = np.full((1, 128), np.finfo(np.float32).max, dtype=np.float32)
+    check(np.concatenate([x, big]), np.concatenate([-x, -big]), "f32", 128)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_blocks_with_infinities_and_nans_stand_for_nans_and_leave_their_neighbours(dtype):
+    rng = np.random.default_rng(5)
+    K, V = rows_of(rng, 40, 128, dtype), rows_of(rng, 40, 128, dtype)
+    K[3, 5], K[7, 127], V[0, 32], V[39, 64] = np.inf, np.nan, -np.inf, np.nan
+    V[9, 10], V[9, 11] = np.inf, -np.inf
+    check(K, V, dtype, 128)
+
+
+def test_units_in_any_order_and_rows_between_them_stay():
+    """Ragged units (more than one launch's list), empty ones among them, gaps on both sides, destinations not ascending."""
+    import torch
+    import paper_2603_00907_amd as kvs
+    rng = np.random.default_rng(6)
+    D, lens = 64, [int(x) for x in rng.integers(0, 40, 150)]
+    src, acc = [], 0
+    for l in lens:
+        src.append(acc)
+        acc += l + 2
+    dst, at = [0] * len(lens), 5
+    for u in rng.permutation(len(lens)):
+        dst[u] = at
+        at += lens[u] + int(rng.integers(0, 3))
+    K, V = rows_of(rng, acc, D, "f32"), rows_of(rng, acc, D, "f32")
+    p = kvs.Problem(lens=lens, budgets=[1] * len(lens), group=1, window=1, head_dim=D, dtype="f32", in_rows=src, out_rows=dst)
+    buf = packed_buffers(at + 8, D)
+    kvs.kvs_pack(p, to_device(K, "f32"), to_device(V, "f32"), *buf, stream=torch.cuda.current_stream().cuda_stream)
+    got = [b.cpu().numpy() for b in buf]
+    want = [np.full(b.shape, 0xA5, dtype=np.uint8) for b in got]
+    for n, s, d in zip(lens, src, dst):
+        if n:
+            want[0][d:d + n], want[1][d:d + n] = R.pack(K[s:s + n])
+            want[2][d:d + n], want[3][d:d + n] = R.pack(V[s:s + n])
+    for g, w in zip(got, want):
+        assert (g == w).all()
+    # and back to where the rows came from: the gaps keep what they hold
+    back = kvs.Problem(lens=lens, budgets=[1] * len(lens), group=1, window=1, head_dim=D, dtype="f32", in_rows=dst, out_rows=src)
+    out = [torch.full((acc + 3, D), 512.0, device="cuda") for _ in range(2)]
+    kvs.kvs_unpack(back, *buf, *out, stream=torch.cuda.current_stream().cuda_stream)
+    for o, (c, s) in zip(out, (got[:2], got[2:])):
+        want_rows = np.full((acc + 3, D), 512.0)
+        for n, a, b in zip(lens, src, dst):
+            want_rows[a:a + n] = R.unpack(c[b:b + n], s[b:b + n])
+        assert (o.cpu().numpy() == want_rows).all()
+
+
+@pytest.mark.parametrize("units,n", [(256, 1), (70000, 1), (300, 3)])
+def test_equal_units_of_few_rows(units, n):
+    """A step's new rows of all caches: appended at the end of each cache."""
+    import torch
+    import paper_2603_00907_amd as kvs
+    rng = np.random.default_rng(7)
+    D, room = 64, n + 2
+    K, V = rows_of(rng, units * n, D, "bf16"), rows_of(rng, units * n, D, "bf16")
+    p = kvs.Problem(lens=[n] * units, budgets=[n] * units, group=1, window=1, head_dim=D, dtype="bf16",
+                    out_rows=[u * room + 1 for u in range(units)])
+    buf = packed_buffers(units * room, D)
+    kvs.kvs_pack(p, to_device(K, "bf16"), to_device(V, "bf16"), *buf, stream=torch.cuda.current_stream().cuda_stream)
+    for x, codes, scales in ((K, buf[0], buf[1]), (V, buf[2], buf[3])):
+        for got, want in zip((codes, scales), R.pack(x)):
+            got = got.cpu().numpy().reshape(units, room, -1)
+            assert (got[:, 1:1 + n] == want.reshape(units, n, -1)).all()
+            assert (got[:, 0] == 0xA5).all() and (got[:, 1 + n:] == 0xA5).all()
