@@ -25,7 +25,7 @@ OBJ = os.path.join(HERE, "_build")
 SOURCES = ["kvs_api.hip", "kvs_score_valu.hip", "kvs_score_mfma.hip", "kvs_score_shared.hip", "kvs_score_split.hip",
            "kvs_score_fused.hip", "kvs_select.hip", "kvs_merge.hip", "kvs_decode.hip",
            "kvs_perquery.hip", "kvs_perquery_f32.hip", "kvs_table.hip", "kvs_window_api.hip", "kvs_window_rows.hip",
-           "kvs_pack.hip"]
+           "kvs_window_tiles.hip", "kvs_pack.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,7 +1,7 @@
 // Shared by the host layer and the kernels of the masked attention over a cache (kvs_window_attention and its _packed form).
 #pragma once
 
-#include "kvs_device.h"
+#include "kvs_fp4.h"
 
 namespace kvs {
 
@@ -46,6 +46,7 @@ struct Cache {
 
 constexpr int kMaxParts = 256;           // pieces that the rows of a unit are cut into at most
 constexpr int kWindowTile = 32;          // cache rows per tile of the kernels in kvs_window_rows.hip
+constexpr int kWideTile = 64;            // and of those in kvs_window_tiles.hip
 
 struct WindowShape {
   int R, G, W, D;
@@ -102,10 +103,40 @@ __device__ __forceinline__ size_t query_row(const WindowShape& sh, int unit, int
 
 enum class CacheKind { kF32, kBf16, kPackedF32, kPackedBf16 };   // the cache, and the type of Q and out
 
+// Four neighbouring values of a row from channel ch on (a multiple of four), wherever speed does not matter.
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+template <CacheKind KIND, int D>
+__device__ __forceinline__ f32x4_t four_values(const Cache& cache, size_t row, int ch) {
+  const size_t at = row * D + ch;
+  if constexpr (KIND == CacheKind::kF32) {
+    return *(const f32x4_t*)((const float*)cache.v + at);
+  } else if constexpr (KIND == CacheKind::kBf16) {
+    const uint2 x = *(const uint2*)((const uint16_t*)cache.v + at);
+    return f32x4_t{bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y)};
+  } else {
+    const uint32_t x = *(const uint16_t*)((const uint8_t*)cache.v + at / 2);
+    const float sc = fp4::scale_of(cache.vs[at / fp4::kBlock]);
+    const uint32_t a = fp4::two_of<0>(x, sc), b = fp4::two_of<1>(x, sc);
+    return f32x4_t{bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)};
+  }
+}
+// A numerator over its denominator; zero where no term was seen.
+__device__ __forceinline__ float quotient(float num, float den) { return den == 0.f ? 0.f : num / den; }
+// The running maximum of a softmax is raised only when a logit exceeds it by this many powers of two: terms of up to 2^8 are
+// as exact as terms of up to 1.
+constexpr float kSlack = 8.f;
+
 // The launchers: `equal` or, where it is null, `listed`.
 hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
                               CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
                               hipStream_t stream);
+// bf16 outputs, blocks of 128 or 256 query rows (kvs_window_tiles.hip).
+hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
+                               CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
+                               hipStream_t stream);
+// out from the partial results of kernels whose tiles have `tile` rows (kWindowTile or kWideTile).
+hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
+                                bool f32, int tile, const float* part, void* out, hipStream_t stream);
 // Descriptors of the units from `first` on into the workspace.
 hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, CacheUnit* dst, hipStream_t stream);
 

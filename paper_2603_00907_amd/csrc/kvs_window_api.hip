@@ -49,8 +49,12 @@ kvs_status launched(hipError_t e, const char* what) {
 }
 
 // ---- attention
+#ifndef KVS_WIDE_BLOCK
+#define KVS_WIDE_BLOCK 128
+#endif
 struct WindowPlan {
   WindowShape sh{};
+  bool wide = false;           // kvs_window_tiles.hip, else kvs_window_rows.hip
   bool equal = false;          // units of one length at equal distances
   size_t part_bytes = 0, table_bytes = 0;
   size_t bytes() const { return part_bytes + table_bytes; }
@@ -66,21 +70,22 @@ long long tiles_bound(const WindowShape& sh, int len, int tile) {
 
 // How the rows that a block sees are cut into pieces: workgroups enough for the chip, and pieces long enough for what a
 // workgroup does once.
-void cut_into_parts(const kvs_problem* p, WindowShape& sh) {
-  constexpr long long kWanted = 1024, kLeastTiles = 8;
+void cut_into_parts(const kvs_problem* p, bool wide, WindowShape& sh) {
+  const long long wanted = wide ? 512 : 1024, least = wide ? 4 : 8;
   long long total = 0, most = 1;
   for (int u = 0; u < p->n_units; ++u) {
-    const long long t = tiles_bound(sh, p->len[u], kWindowTile);
+    const long long t = tiles_bound(sh, p->len[u], wide ? kWideTile : kWindowTile);
     total += t * sh.n_blocks;
     most = std::max(most, t);
   }
-  long long per = std::max((total + kWanted - 1) / kWanted, kLeastTiles);
+  long long per = std::max((total + wanted - 1) / wanted, least);
+  if (wide && (long long)p->n_units * sh.n_blocks >= wanted) per = most;
   per = std::max(per, (most + kMaxParts - 1) / kMaxParts);
   sh.part_tiles = (int)per;
   sh.n_parts = (int)((most + per - 1) / per);
 }
 
-kvs_status make_window_plan(const kvs_problem* p, int32_t span, WindowPlan* plan, int* elt) {
+kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, WindowPlan* plan, int* elt) {
   const kvs_status st = check_common(p, elt);
   if (st != KVS_OK) return st;
   if (p->group < 1 || p->window < 1 || (long long)p->group * p->window > KVS_MAX_WINDOW_ROWS) return KVS_ERR_INVALID_ARG;
@@ -96,9 +101,10 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, WindowPlan* plan
   sh.sinks = std::min(p->n_sink, KVS_MAX_LEN);
   const double scale = p->scale == 0.f ? 1.0 / std::sqrt((double)p->head_dim) : (double)p->scale;
   sh.scale_log2 = (float)(scale * 1.4426950408889634);
-  sh.block = sh.R <= 16 ? 16 : sh.R <= 32 ? 32 : 64;
+  plan->wide = *elt == 2 && !packed && sh.R > 64;
+  sh.block = plan->wide ? KVS_WIDE_BLOCK : sh.R <= 16 ? 16 : sh.R <= 32 ? 32 : 64;
   sh.n_blocks = (sh.R + sh.block - 1) / sh.block;
-  cut_into_parts(p, sh);
+  cut_into_parts(p, plan->wide, sh);
   plan->equal = true;
   for (int u = 1; u < p->n_units; ++u) {
     plan->equal = plan->equal && p->len[u] == p->len[0] && p->in_row[u] - p->in_row[u - 1] == p->in_row[1] - p->in_row[0];
@@ -122,7 +128,7 @@ kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, con
                             void* ws, size_t ws_bytes, void* hip_stream) {
   WindowPlan plan;
   int elt = 0;
-  kvs_status st = make_window_plan(p, span, &plan, &elt);
+  kvs_status st = make_window_plan(p, span, packed, &plan, &elt);
   if (st != KVS_OK) return st;
   const WindowShape& sh = plan.sh;
   if (plan.bytes() > 0 && (ws == nullptr || ((uintptr_t)ws % kAlign) != 0 || ws_bytes < plan.bytes())) return KVS_ERR_WORKSPACE;
@@ -153,6 +159,7 @@ kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, con
   }
   const CacheKind kind = elt == 4 ? (packed ? CacheKind::kPackedF32 : CacheKind::kF32)
                                   : (packed ? CacheKind::kPackedBf16 : CacheKind::kBf16);
+  const auto launch = plan.wide ? launch_window_tiles : launch_window_rows;
   // (a call of more workgroups than a grid may have goes out in several launches)
   const long long groups = std::max<long long>((long long)sh.n_blocks * sh.n_parts, sh.n_parts > 1 ? sh.R : 1);
   const int most = (int)std::max<long long>(1, kMostGroups / groups);
@@ -161,12 +168,12 @@ kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, con
     if (plan.equal) {
       const long long step = p->n_units > 1 ? p->in_row[1] - p->in_row[0] : 0;
       const EqualUnits units = {p->in_row[first], step, p->len[0], first};
-      e = launch_window_rows(&units, nullptr, n, sh, kind, cache, Q, out, part, s);
+      e = launch(&units, nullptr, n, sh, kind, cache, Q, out, part, s);
     } else {
       ListedUnits units;
       units.ext = table ? table + first : nullptr;
       for (int i = 0; i < kInlineUnits; ++i) units.u[i] = cache_unit(p, first + std::min(i, n - 1));
-      e = launch_window_rows(nullptr, &units, n, sh, kind, cache, Q, out, part, s);
+      e = launch(nullptr, &units, n, sh, kind, cache, Q, out, part, s);
     }
   }
   return launched(e, "an attention launch");
@@ -256,11 +263,15 @@ extern "C" {
 
 kvs_status kvs_window_attention_workspace_size(const kvs_problem* p, int32_t span, size_t* bytes) {
   if (bytes == nullptr) return KVS_ERR_INVALID_ARG;
-  WindowPlan plan;
-  int elt = 0;
-  const kvs_status st = make_window_plan(p, span, &plan, &elt);
-  if (st != KVS_OK) return st;
-  *bytes = plan.bytes();
+  size_t most = 0;                             // (one size for both forms)
+  for (const bool packed : {false, true}) {
+    WindowPlan plan;
+    int elt = 0;
+    const kvs_status st = make_window_plan(p, span, packed, &plan, &elt);
+    if (st != KVS_OK) return st;
+    most = std::max(most, plan.bytes());
+  }
+  *bytes = most;
   return KVS_OK;
 }
 

@@ -35,8 +35,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = kWindowTile;
-// The running maximum is raised only when a logit exceeds it by this many powers of two: terms up to 2^8 are as exact.
-constexpr float kSlack = 8.f;
 
 // A piece of a unit's rows (at most 2^31 bytes of them): one scalar base, 32-bit offsets.
 template <typename T>
@@ -90,10 +88,6 @@ struct Rows<CacheKind::kBf16, D> {
   __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
     v[i] = at<vpiece>((const char*)cache.v + row0 * (2 * D), row * (2 * D) + c * (D / 8));
   }
-  static __device__ __forceinline__ f32x4 four_values(const Cache& cache, size_t row0, uint32_t row, int ch) {
-    const uint2 x = at<uint2>((const char*)cache.v + row0 * (2 * D), row * (2 * D) + 2 * ch);
-    return f32x4{bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y)};
-  }
   __device__ __forceinline__ bf16x8 key(int h, int s) const { return __builtin_bit_cast(bf16x8, k[h][s]); }
   // channels 2 W, 2 W + 1 of the lane's
   template <int W> __device__ __forceinline__ uint32_t value(int i) const { return v[i][W]; }
@@ -120,12 +114,6 @@ struct PackedRows {
   __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
     v[i] = at<vpiece>((const char*)cache.v + row0 * (D / 2), row * (D / 2) + c * (D / 32));
     vs[i] = at<uint8_t>((const char*)cache.vs + row0 * (D / 32), row * (D / 32) + c * CPL / 32);
-  }
-  static __device__ __forceinline__ f32x4 four_values(const Cache& cache, size_t row0, uint32_t row, int ch) {
-    const uint32_t x = at<uint16_t>((const char*)cache.v + row0 * (D / 2), row * (D / 2) + ch / 2);
-    const float sc = scale_of(at<uint8_t>((const char*)cache.vs + row0 * (D / 32), row * (D / 32) + ch / 32));
-    const uint32_t a = two_of<0>(x, sc), b = two_of<1>(x, sc);
-    return f32x4{bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)};
   }
   __device__ __forceinline__ bf16x8 key(int h, int s) const {
     const float sc = scale_of(ks[h]);
@@ -155,9 +143,6 @@ struct Rows<CacheKind::kF32, D> {
     const char* base = (const char*)cache.v + row0 * (4 * D);
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) v[i][e] = at<f32x4>(base, row * (4 * D) + 16 * c + 256 * e);
-  }
-  static __device__ __forceinline__ f32x4 four_values(const Cache& cache, size_t row0, uint32_t row, int ch) {
-    return at<f32x4>((const char*)cache.v + row0 * (4 * D), row * (4 * D) + 4 * ch);
   }
 };
 
@@ -202,8 +187,6 @@ __device__ __forceinline__ void store_two(T* at, float a, float b) {
   if constexpr (std::is_same_v<T, float>) *(float2*)at = make_float2(a, b);
   else *(uint32_t*)at = cvt_pk_bf16(a, b);
 }
-// A numerator over its denominator; zero where no term was seen.
-__device__ __forceinline__ float quotient(float num, float den) { return den == 0.f ? 0.f : num / den; }
 
 template <CacheKind KIND, int D, int NQ, typename Tab>
 __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void window_rows_kernel(
@@ -415,7 +398,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void windo
           for (int j4 = 0; j4 < NJ / 4; ++j4) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-              const f32x4 y = L::four_values(cache, un.in_row, t, channel_of<F32, D>(j4, 4 * g + v));
+              const f32x4 y = four_values<KIND, D>(cache, un.in_row + t, channel_of<F32, D>(j4, 4 * g + v));
 #pragma unroll
               for (int n = 0; n < NQ; ++n) {
                 const bool seen = sees(sh, pos[n], t);
@@ -536,7 +519,6 @@ __global__ __launch_bounds__(256) void cache_unit_table_kernel(const CacheUnitBa
 template <CacheKind KIND, int D, typename Tab>
 hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
                        float* part, hipStream_t stream) {
-  typedef typename Rows<KIND, D>::Io Io;
   const dim3 grid((unsigned)((long long)n_units * sh.n_blocks * sh.n_parts));
   auto go = [&](auto nq) {
     hipLaunchKernelGGL((window_rows_kernel<KIND, D, decltype(nq)::value, Tab>), grid, dim3(kThreads), 0, stream, tab, sh,
@@ -545,10 +527,6 @@ hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const
   if (sh.block == 16) go(std::integral_constant<int, 1>{});
   else if (sh.block == 32) go(std::integral_constant<int, 2>{});
   else go(std::integral_constant<int, 4>{});
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || sh.n_parts == 1) return e;
-  hipLaunchKernelGGL((window_reduce_kernel<Io, D, kTile, Tab>), dim3((unsigned)((long long)n_units * sh.R)), dim3(kThreads),
-                     0, stream, tab, sh, part, out);
   return hipGetLastError();
 }
 
@@ -575,8 +553,31 @@ hipError_t launch_tab(const Tab& tab, int n_units, const WindowShape& sh, CacheK
 hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
                               CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
                               hipStream_t stream) {
-  if (equal) return launch_tab(*equal, n_units, sh, kind, cache, Q, out, part, stream);
-  return launch_tab(*listed, n_units, sh, kind, cache, Q, out, part, stream);
+  const hipError_t e = equal ? launch_tab(*equal, n_units, sh, kind, cache, Q, out, part, stream)
+                             : launch_tab(*listed, n_units, sh, kind, cache, Q, out, part, stream);
+  if (e != hipSuccess || sh.n_parts == 1) return e;
+  const bool f32 = kind == CacheKind::kF32 || kind == CacheKind::kPackedF32;
+  return launch_window_reduce(equal, listed, n_units, sh, f32, kTile, part, out, stream);
+}
+
+hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
+                                bool f32, int tile, const float* part, void* out, hipStream_t stream) {
+  auto go = [&](const auto& tab, auto io, auto d, auto t) {
+    hipLaunchKernelGGL((window_reduce_kernel<decltype(io), decltype(d)::value, decltype(t)::value, std::decay_t<decltype(tab)>>),
+                       dim3((unsigned)((long long)n_units * sh.R)), dim3(kThreads), 0, stream, tab, sh, part, out);
+  };
+  auto typed = [&](const auto& tab, auto d) {
+    if (f32) go(tab, float{}, d, std::integral_constant<int, kWindowTile>{});
+    else if (tile == kWindowTile) go(tab, uint16_t{}, d, std::integral_constant<int, kWindowTile>{});
+    else go(tab, uint16_t{}, d, std::integral_constant<int, kWideTile>{});
+  };
+  auto sized = [&](const auto& tab) {
+    if (sh.D == 64) typed(tab, std::integral_constant<int, 64>{});
+    else typed(tab, std::integral_constant<int, 128>{});
+  };
+  if (equal) sized(*equal);
+  else sized(*listed);
+  return hipGetLastError();
 }
 
 hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, CacheUnit* dst, hipStream_t stream) {
