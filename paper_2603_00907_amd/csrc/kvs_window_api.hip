@@ -49,9 +49,6 @@ kvs_status launched(hipError_t e, const char* what) {
 }
 
 // ---- attention
-#ifndef KVS_WIDE_BLOCK
-#define KVS_WIDE_BLOCK 128
-#endif
 struct WindowPlan {
   WindowShape sh{};
   bool wide = false;           // kvs_window_tiles.hip, else kvs_window_rows.hip
@@ -71,7 +68,7 @@ long long tiles_bound(const WindowShape& sh, int len, int tile) {
 // How the rows that a block sees are cut into pieces: workgroups enough for the chip, and pieces long enough for what a
 // workgroup does once.
 void cut_into_parts(const kvs_problem* p, bool wide, WindowShape& sh) {
-  const long long wanted = wide ? 512 : 1024, least = wide ? 4 : 8;
+  const long long wanted = wide ? 256 : 1024, least = wide ? 4 : 8;
   long long total = 0, most = 1;
   for (int u = 0; u < p->n_units; ++u) {
     const long long t = tiles_bound(sh, p->len[u], wide ? kWideTile : kWindowTile);
@@ -102,7 +99,7 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
   const double scale = p->scale == 0.f ? 1.0 / std::sqrt((double)p->head_dim) : (double)p->scale;
   sh.scale_log2 = (float)(scale * 1.4426950408889634);
   plan->wide = *elt == 2 && !packed && sh.R > 64;
-  sh.block = plan->wide ? KVS_WIDE_BLOCK : sh.R <= 16 ? 16 : sh.R <= 32 ? 32 : 64;
+  sh.block = plan->wide ? (sh.R <= 128 ? 128 : 256) : sh.R <= 16 ? 16 : sh.R <= 32 ? 32 : 64;
   sh.n_blocks = (sh.R + sh.block - 1) / sh.block;
   cut_into_parts(p, plan->wide, sh);
   plan->equal = true;

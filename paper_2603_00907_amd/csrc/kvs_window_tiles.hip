@@ -8,8 +8,10 @@
 //   O^T[d, q] += V^T P: P is in operand order as it leaves the softmax, rounded to one bf16 number (its error, at most 2^-9 of
 //             each weight and of any sign, disappears in the sum beside the rounding of the output), and V^T comes from LDS by
 //             transposing reads.
-// The products of tile j + 1 with Q are issued beside the exponentials of tile j.  One barrier per tile: while tile j is worked
-// on, K of tile j + 2 and V of tile j + 1 travel through registers into the halves of LDS that nobody reads.
+// The next 32 rows' products with Q are issued beside the exponentials of the 32 rows at hand.  One barrier per tile: while
+// tile j is worked on, K of tile j + 2 and V of tile j + 1 travel from memory into those of the six buffers in LDS that
+// nobody reads.  (Six arrays, and every access to one that is known at compile time: the compiler then waits for a load into LDS where its
+// array is read, and not at every read.)
 // Pieces of 16 bytes are swizzled within a row of LDS so that neither kind of read meets a bank twice.
 #include <type_traits>
 
@@ -24,9 +26,11 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kTile = kWideTile;
+// A lane's sixteen terms may add up to this before their reference is raised to the largest logit.
+constexpr float kMostSum = 65536.f;
 
 // Where piece `p` (16 bytes) of row r is within its row.
 template <int D> __device__ __forceinline__ int key_slot(int r, int p) { return D == 128 ? p ^ (r % 16) : p ^ (r / 2 % 8); }
@@ -47,17 +51,18 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 x, bool& odd) {
 
 __device__ __forceinline__ float of_both_halves_max(float x) { return fmaxf(x, __shfl_xor(x, 32, kWave)); }
 
-template <CacheKind KIND, int D, int NB, bool COUNTS, typename Tab>
-__global__ __launch_bounds__(kThreads, NB == 1 ? 2 : 1) void window_tiles_kernel(
+template <CacheKind KIND, int D, int WAVES, bool COUNTS, typename Tab>
+__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 1) void window_tiles_kernel(
     const Tab tab, const WindowShape sh, const Cache cache, int n_units, const uint16_t* __restrict__ Q,
     uint16_t* __restrict__ out, float* __restrict__ part) {
+  constexpr int kThreads = WAVES * kWave;
   constexpr int KS = D / 16;                // steps of the contraction over channels
   constexpr int DB = D / 32;                // blocks of 32 channels
   constexpr int PPR = D / 8;                // pieces per row
   constexpr int PER = kTile * PPR / kThreads;    // pieces per thread of a tile of K, and of V
-  __shared__ u32x4 sm_k[2][kTile * PPR];
-  __shared__ u32x4 sm_v[2][kTile * PPR];
-  __shared__ __attribute__((aligned(16))) float sm_cnt[2][kTile];
+  __shared__ u32x4 sm_k[2][kTile * PPR], sm_v[2][kTile * PPR];
+  // cardinalities as pairs hi + lo of bf16 numbers (exact up to 65536, to 2^-17 beyond): of four rows both hi pairs, then both lo
+  __shared__ u32x4 sm_cnt[2][kTile / 4];
 
   // A unit's workgroups are n_units apart, which puts them on one XCD where n_units is a multiple of eight, and the last
   // blocks, which see most under a causal mask, come first.
@@ -70,23 +75,14 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 2 : 1) void window_tiles_kernel
   const int j0 = piece * sh.part_tiles, j1 = min(re.tiles, j0 + sh.part_tiles);
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
   const int col = lane % 32, half = lane / 32;
-  const int row0 = block * sh.block + wave * 32 * NB;          // the wavefront's first query row
+  const int row = block * sh.block + wave * 32 + col;          // the lane's query row
+  const int pos = sh.causal ? un.len - sh.W + min(row, sh.R - 1) / sh.G : un.len - 1;
+  const int pos_min = __builtin_amdgcn_readfirstlane(pos), pos_max = __builtin_amdgcn_readlane(pos, 31);
 
-  int pos[NB];
+  f32x16 acc[DB];
+  float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int n = 0; n < NB; ++n) pos[n] = sh.causal ? un.len - sh.W + min(row0 + 32 * n + col, sh.R - 1) / sh.G : un.len - 1;
-  const int pos_min = __builtin_amdgcn_readfirstlane(pos[0]);
-  const int pos_max = __builtin_amdgcn_readlane(pos[NB - 1], 31);
-
-  f32x16 acc[NB][DB];
-  float m[NB], l[NB];
-#pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    m[n] = -INFINITY;
-    l[n] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) acc[n][d] = f32x16{};
-  }
+  for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
   bool odd = false;                         // a value that is not finite was left out
 
   auto start_of = [&](int t) { return t < re.sink_tiles ? t * kTile : re.first + (t - re.sink_tiles) * kTile; };
@@ -97,187 +93,195 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 2 : 1) void window_tiles_kernel
   };
 
   if (j0 < j1) {
-    bf16x8 q[NB][KS];
+    bf16x8 q[KS];
+    const uint16_t* src = Q + query_row(sh, un.index, min(row, sh.R - 1)) * D + 8 * half;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const uint16_t* src = Q + query_row(sh, un.index, min(row0 + 32 * n + col, sh.R - 1)) * D + 8 * half;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) q[n][k] = *(const bf16x8*)(src + 16 * k);
-    }
+    for (int k = 0; k < KS; ++k) q[k] = *(const bf16x8*)(src + 16 * k);
     const char* kbase = (const char*)cache.k + (size_t)un.in_row * (2 * D);
     const char* vbase = (const char*)cache.v + (size_t)un.in_row * (2 * D);
     const int32_t* counts = COUNTS ? cache.counts + un.in_row : nullptr;
+    // A tile travels through registers: requested when a tile is begun, written to LDS when that one is nearly done.
+    // (Rows past the range's end repeat the last one.)
     const int srow = tid / PPR, spiece = tid % PPR;
-    // (rows past the range's end repeat the last one)
-    auto load = [&](const char* base, int t, u32x4 (&r)[PER]) {
-      const int t0 = start_of(t), last = end_of(t) - 1;
+    u32x4 rk[PER], rv[PER];
+    float rc = 1.f;
+    const uint32_t soffset = srow * (2 * D) + 16 * spiece;
+    auto request = [&](const char* base, int t, u32x4 (&r)[PER]) __attribute__((always_inline)) {
+      const int t0 = start_of(t), last = end_of(t) - 1 - t0;
+      const char* first = base + (uint32_t)t0 * (2 * D);
+      if (last >= kTile - 1) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        r[i] = *(const u32x4*)(base + (uint32_t)(min(t0 + srow + i * (kThreads / PPR), last) * (2 * D) + 16 * spiece));
+        for (int i = 0; i < PER; ++i) r[i] = *(const u32x4*)(first + i * (kThreads / PPR) * (2 * D) + soffset);
+      } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          r[i] = *(const u32x4*)(first + (uint32_t)(min(srow + i * (kThreads / PPR), last) * (2 * D) + 16 * spiece));
+      }
     };
-    auto store_keys = [&](int b, const u32x4 (&r)[PER]) {
+    auto request_values = [&](int t) __attribute__((always_inline)) {
+      request(vbase, t, rv);
+      if (COUNTS && tid < kTile) rc = (float)counts[start_of(t) + min(tid, end_of(t) - 1 - start_of(t))];
+    };
+    auto store_keys = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int row = srow + i * (kThreads / PPR);
-        sm_k[b][row * PPR + key_slot<D>(row, spiece)] = r[i];
+        sm_k[b][row * PPR + key_slot<D>(row, spiece)] = rk[i];
       }
     };
-    auto store_values = [&](int b, int t, u32x4 (&r)[PER]) {
+    auto store_values = [&](int t, int b) __attribute__((always_inline)) {
       if (!seen_whole(start_of(t), end_of(t), re.pos_min, re.pos_max)) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) r[i] = finite_only(r[i], odd);
+        for (int i = 0; i < PER; ++i) rv[i] = finite_only(rv[i], odd);
       }
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int row = srow + i * (kThreads / PPR);
-        sm_v[b][row * PPR + value_slot<D>(row, spiece)] = r[i];
+        sm_v[b][row * PPR + value_slot<D>(row, spiece)] = rv[i];
+      }
+      if (COUNTS && tid < kTile) {
+        const uint32_t hi = cvt_pk_bf16(rc, 0.f);
+        uint16_t* at = (uint16_t*)&sm_cnt[b][tid / 4] + tid % 4;
+        at[0] = (uint16_t)hi;
+        at[4] = (uint16_t)cvt_pk_bf16(rc - bf16_lo(hi), 0.f);
       }
     };
-    auto load_count = [&](int t) {
-      return COUNTS && tid < kTile ? (float)counts[min(start_of(t) + tid, end_of(t) - 1)] : 1.f;
+    // K operands of half a of the tile in buffer b, and V^T operands of its rows 16 st ..: element i of the one of channels
+    // 32 d .. is row 16 st + 8 (i / 4) + 4 half + i % 4
+    bf16x8 kf[KS];
+    auto read_keys = [&](int b, int a) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        kf[k] = __builtin_bit_cast(bf16x8, sm_k[b][(32 * a + col) * PPR + key_slot<D>(col, 2 * k + half)]);
     };
-
-    f32x16 s[NB][2];
-    auto products_with_keys = [&](int b, f32x16 (&to)[NB][2]) {
-#pragma unroll
-      for (int n = 0; n < NB; ++n) to[n][0] = to[n][1] = f32x16{};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const bf16x8 key = __builtin_bit_cast(bf16x8, sm_k[b][(32 * a + col) * PPR + key_slot<D>(col, 2 * k + half)]);
-#pragma unroll
-          for (int n = 0; n < NB; ++n) to[n][a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[n][k], to[n][a], 0, 0, 0);
-        }
-      }
-    };
-
-    // V^T operand of channels 32 d .. and of rows 16 st ..: element i is row 16 st + 8 (i / 4) + 4 half + i % 4
     const int vrow = 4 * half + lane % 16 / 4, vpiece = 2 * (lane / 16 % 2) + lane % 4 / 2;
-    auto value_operand = [&](int b, int st, int d) {
-      s16x8 x;
+    auto value_operand = [&](int b, int st, int d) __attribute__((always_inline)) {
+      s16x4 x[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const short* at = (const short*)&sm_v[b][(16 * st + 8 * h + vrow) * PPR + value_slot<D>(vrow, 4 * d + vpiece)];
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + lane % 2 * 4));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * h + i] = y[i];
+        x[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + lane % 2 * 4));
       }
-      return __builtin_bit_cast(bf16x8, x);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto products_with_keys = [&](f32x16& to) __attribute__((always_inline)) {
+      to = f32x16{};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[k], to, 0, 0, 0);
     };
 
-    u32x4 rk[PER], rv[PER];
-    {
-      load(kbase, j0, rk);
-      load(vbase, j0, rv);
-      const float c = load_count(j0);
-      store_keys(0, rk);
-      if (j0 + 1 < j1) load(kbase, j0 + 1, rk);
-      store_values(0, j0, rv);
-      if (COUNTS && tid < kTile) sm_cnt[0][tid] = c;
-      if (j0 + 1 < j1) store_keys(1, rk);
-    }
-    __syncthreads();
-    products_with_keys(0, s);
-
-    auto tile = [&](int j, auto last_c) {
-      constexpr bool LAST = decltype(last_c)::value;
-      const int b = (j - j0) & 1;
-      float next_count = 1.f;
-      if (!LAST) {
-        load(vbase, j + 1, rv);
-        next_count = load_count(j + 1);
-        if (j + 2 < j1) load(kbase, j + 2, rk);
-      }
+    // Half A of tile j (buffer B), whose logits are in s.  On the way: the products of the K operands that are in kf, the next
+    // half's, to s2, and the operands of the half after that.
+    auto step = [&](auto half_c, auto buffer_c, int j, f32x16& s, f32x16& s2) __attribute__((always_inline)) {
+      constexpr int A = decltype(half_c)::value, B = decltype(buffer_c)::value;
       const int t0 = start_of(j), end = end_of(j);
       if (!seen_whole(t0, end, pos_min, pos_max)) {
+        // row 32 A + x of the tile for x = 8 (v / 4) + v % 4 plus this: limits that x is compared with
+        const int base = t0 + 32 * A + 4 * half;
+        const int before_end = end - base, before_sinks = sh.sinks - base;
+        const int last = min(pos - base, before_end - 1);
+        const int hidden = sh.span > 0 ? pos - sh.span - base : -1 - base;       // rows up to here are seen as sinks only
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-#pragma unroll
-          for (int a = 0; a < 2; ++a) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              const int t = t0 + 32 * a + 8 * (v / 4) + 4 * half + v % 4;
-              s[n][a][v] = t < end && sees(sh, pos[n], t) ? s[n][a][v] : -INFINITY;
-            }
-          }
+        for (int v = 0; v < 16; ++v) {
+          const int x = 8 * (v / 4) + v % 4;
+          const bool seen = (x <= last) & ((x > hidden) | (x < before_sinks));
+          s[v] = seen ? s[v] : -INFINITY;
         }
       }
-      float ref[NB];
+      bf16x8 vf[DB];
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        float top = -INFINITY;
+      for (int d = 0; d < DB; ++d) vf[d] = value_operand(B, 2 * A, d);
+      products_with_keys(s2);
+      uint32_t p[8];
+      float sum;
+      auto terms = [&](float ref) __attribute__((always_inline)) {
+        float x[16];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) top = fmaxf(fmaxf(top, s[n][0][v]), s[n][1][v]);
-        top *= sh.scale_log2;
-        if (__ballot(top > m[n] + kSlack) != 0) {            // rare after the first tiles
-          top = fmaxf(of_both_halves_max(top), m[n]);
-          const float corr = m[n] == top ? 1.f : __builtin_amdgcn_exp2f(m[n] - top);
-          l[n] *= corr;
+        for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(fmaf(s[v], sh.scale_log2, -ref));
 #pragma unroll
-          for (int d = 0; d < DB; ++d) {
+        for (int i = 0; i < 8; ++i) p[i] = cvt_pk_bf16(x[2 * i], x[2 * i + 1]);
+        // (of the terms as they enter the product with V)
+        sum = 0.f;
+        auto add = [&](uint32_t x, uint32_t y) {
+          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), sum, false);
+        };
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[n][d][v] *= corr;
-          }
-          m[n] = top;
-        }
-        ref[n] = m[n] == -INFINITY ? 0.f : m[n];             // (a query that has seen nothing yet)
-      }
-      // the next tile's products and this one's exponentials
-      f32x16 s2[NB][2];
-      if (!LAST) products_with_keys(b ^ 1, s2);
-      bf16x8 p[NB][4];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        float sum = 0.f;
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          float x[16];
-#pragma unroll
-          for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_exp2f(fmaf(s[n][a][v], sh.scale_log2, -ref[n]));
-#pragma unroll
-          for (int v4 = 0; v4 < 4; ++v4) {
-            if (COUNTS) {                                    // c copies of the slot in the denominator
-              const float4 c4 = *(const float4*)&sm_cnt[b][32 * a + 8 * v4 + 4 * half];
-              sum = fmaf(c4.x, x[4 * v4], sum);
-              sum = fmaf(c4.y, x[4 * v4 + 1], sum);
-              sum = fmaf(c4.z, x[4 * v4 + 2], sum);
-              sum = fmaf(c4.w, x[4 * v4 + 3], sum);
-            } else {
-              sum += (x[4 * v4] + x[4 * v4 + 1]) + (x[4 * v4 + 2] + x[4 * v4 + 3]);
-            }
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = cvt_pk_bf16(x[8 * h + 2 * i], x[8 * h + 2 * i + 1]);
-            p[n][2 * a + h] = __builtin_bit_cast(bf16x8, w);
+        for (int v4 = 0; v4 < 4; ++v4) {
+          if (COUNTS) {                                      // c copies of the slot in the denominator
+            const u32x4 c4 = sm_cnt[B][8 * A + 2 * v4 + half];
+            add(p[2 * v4], c4[0]);
+            add(p[2 * v4 + 1], c4[1]);
+            add(p[2 * v4], c4[2]);
+            add(p[2 * v4 + 1], c4[3]);
+          } else {
+            add(p[2 * v4], 0x3f803f80u);                     // (ones)
+            add(p[2 * v4 + 1], 0x3f803f80u);
           }
         }
-        l[n] += sum;
-      }
+      };
+      terms(m);
+      if (__ballot(!(sum <= kMostSum)) != 0) {
+        // The reference is below the logits by too much (or there is none yet): rare after the first tiles.
+        float top = s[0];
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
+        for (int v = 1; v < 16; ++v) top = fmaxf(top, s[v]);
+        top = fmaxf(of_both_halves_max(top) * sh.scale_log2, m);
+        const float corr = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        l *= corr;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-          const bf16x8 a = value_operand(b, st, d);
 #pragma unroll
-          for (int n = 0; n < NB; ++n) acc[n][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[n][st], acc[n][d], 0, 0, 0);
+          for (int v = 0; v < 16; ++v) acc[d][v] *= corr;
+        }
+        m = top;
+        terms(m == -INFINITY ? 0.f : m);                     // (a query that has seen nothing yet)
+      }
+      l += sum;
+      if (A == 0) read_keys(B ^ 1, 0);
+      else if (j + 1 < j1) read_keys(B ^ 1, 1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 w = {p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]};
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d], __builtin_bit_cast(bf16x8, w), acc[d], 0, 0, 0);
+          if (h == 0) vf[d] = value_operand(B, 2 * A + 1, d);
         }
       }
-      if (!LAST) {
-#pragma unroll
-        for (int n = 0; n < NB; ++n) { s[n][0] = s2[n][0]; s[n][1] = s2[n][1]; }
-        store_values(b ^ 1, j + 1, rv);
-        if (COUNTS && tid < kTile) sm_cnt[b ^ 1][tid] = next_count;
-        if (j + 2 < j1) store_keys(b, rk);
+    };
+
+    request(kbase, j0, rk);
+    request_values(j0);
+    store_keys(0);
+    if (j0 + 1 < j1) request(kbase, j0 + 1, rk);
+    store_values(j0, 0);
+    if (j0 + 1 < j1) store_keys(1);
+    __syncthreads();
+    f32x16 s0, s1;
+    read_keys(0, 0);
+    products_with_keys(s0);
+    read_keys(0, 1);
+
+    // Tile j: the logits of its first half are in s0 and the K operands of its second in kf, and those of the next tile
+    // afterwards (behind the last tile they are of whatever the buffer holds, and nobody looks at them).
+    auto tile = [&](int j, auto buffer_c) __attribute__((always_inline)) {
+      constexpr int B = decltype(buffer_c)::value;
+      if (j + 1 < j1) request_values(j + 1);
+      if (j + 2 < j1) request(kbase, j + 2, rk);
+      step(std::integral_constant<int, 0>{}, buffer_c, j, s0, s1);
+      step(std::integral_constant<int, 1>{}, buffer_c, j, s1, s0);
+      if (j + 1 < j1) {
+        store_values(j + 1, B ^ 1);
+        if (j + 2 < j1) store_keys(B);
         __syncthreads();
       }
     };
-    int j = j0;
-    for (; j + 1 < j1; ++j) tile(j, std::false_type{});
-    tile(j, std::true_type{});
+    for (int j = j0;;) {
+      tile(j, std::integral_constant<int, 0>{});
+      if (++j == j1) break;
+      tile(j, std::integral_constant<int, 1>{});
+      if (++j == j1) break;
+    }
   }
 
   if (__syncthreads_or(odd)) {
@@ -292,12 +296,9 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 2 : 1) void window_tiles_kernel
 #pragma unroll
           for (int v4 = 0; v4 < 4; ++v4) {
             const f32x4_t y = four_values<KIND, D>(cache, un.in_row + t, 32 * d + 8 * v4 + 4 * half);
+            const bool seen = sees(sh, pos, t);
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-              const bool seen = sees(sh, pos[n], t);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[n][d][4 * v4 + e] += seen && !__builtin_isfinite(y[e]) ? y[e] : 0.f;
-            }
+            for (int e = 0; e < 4; ++e) acc[d][4 * v4 + e] += seen && !__builtin_isfinite(y[e]) ? y[e] : 0.f;
           }
         }
       }
@@ -305,46 +306,42 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 2 : 1) void window_tiles_kernel
   }
 
   // element v of block d: channel 32 d + 8 (v / 4) + 4 half + v % 4 of the lane's query
+  const float den = l + __shfl_xor(l, 32, kWave);
+  if (row >= sh.R) return;
+  if (sh.n_parts == 1) {
+    uint16_t* dst = out + query_row(sh, un.index, row) * D + 4 * half;
+    const float inv = quotient(1.f, den);
 #pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    const int row = row0 + 32 * n + col;
-    const float den = l[n] + __shfl_xor(l[n], 32, kWave);
-    if (row >= sh.R) continue;
-    if (sh.n_parts == 1) {
-      uint16_t* dst = out + query_row(sh, un.index, row) * D + 4 * half;
-      const float inv = quotient(1.f, den);
+    for (int d = 0; d < DB; ++d) {
 #pragma unroll
-      for (int d = 0; d < DB; ++d) {
-#pragma unroll
-        for (int v4 = 0; v4 < 4; ++v4) {
-          *(uint2*)(dst + 32 * d + 8 * v4) = make_uint2(cvt_pk_bf16(acc[n][d][4 * v4] * inv, acc[n][d][4 * v4 + 1] * inv),
-                                                        cvt_pk_bf16(acc[n][d][4 * v4 + 2] * inv, acc[n][d][4 * v4 + 3] * inv));
-        }
+      for (int v4 = 0; v4 < 4; ++v4) {
+        *(uint2*)(dst + 32 * d + 8 * v4) = make_uint2(cvt_pk_bf16(acc[d][4 * v4] * inv, acc[d][4 * v4 + 1] * inv),
+                                                      cvt_pk_bf16(acc[d][4 * v4 + 2] * inv, acc[d][4 * v4 + 3] * inv));
       }
-    } else {
-      float* dst = part + part_at(sh, un.index, row, piece);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-#pragma unroll
-        for (int v4 = 0; v4 < 4; ++v4) {
-          *(float2*)(dst + 32 * d + 8 * v4 + 4 * half) = make_float2(acc[n][d][4 * v4], acc[n][d][4 * v4 + 1]);
-          *(float2*)(dst + 32 * d + 8 * v4 + 4 * half + 2) = make_float2(acc[n][d][4 * v4 + 2], acc[n][d][4 * v4 + 3]);
-        }
-      }
-      if (half == 0) *(float2*)(dst + D) = make_float2(m[n], den);
     }
+  } else {
+    float* dst = part + part_at(sh, un.index, row, piece);
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        *(float2*)(dst + 32 * d + 8 * v4 + 4 * half) = make_float2(acc[d][4 * v4], acc[d][4 * v4 + 1]);
+        *(float2*)(dst + 32 * d + 8 * v4 + 4 * half + 2) = make_float2(acc[d][4 * v4 + 2], acc[d][4 * v4 + 3]);
+      }
+    }
+    if (half == 0) *(float2*)(dst + D) = make_float2(m, den);
   }
 }
 
-template <CacheKind KIND, int D, int NB, typename Tab>
-hipError_t launch_nb(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
+template <CacheKind KIND, int D, int WAVES, typename Tab>
+hipError_t launch_waves(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
                      float* part, hipStream_t stream) {
   const dim3 grid((unsigned)((long long)n_units * sh.n_blocks * sh.n_parts));
   if (cache.counts) {
-    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, NB, true, Tab>), grid, dim3(kThreads), 0, stream, tab, sh, cache, n_units,
+    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, WAVES, true, Tab>), grid, dim3(WAVES * kWave), 0, stream, tab, sh, cache, n_units,
                        (const uint16_t*)Q, (uint16_t*)out, part);
   } else {
-    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, NB, false, Tab>), grid, dim3(kThreads), 0, stream, tab, sh, cache, n_units,
+    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, WAVES, false, Tab>), grid, dim3(WAVES * kWave), 0, stream, tab, sh, cache, n_units,
                        (const uint16_t*)Q, (uint16_t*)out, part);
   }
   return hipGetLastError();
@@ -354,11 +351,11 @@ template <CacheKind KIND, typename Tab>
 hipError_t launch_sized(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
                         float* part, hipStream_t stream) {
   if (sh.D == 64) {
-    return sh.block == 128 ? launch_nb<KIND, 64, 1>(tab, n_units, sh, cache, Q, out, part, stream)
-                           : launch_nb<KIND, 64, 2>(tab, n_units, sh, cache, Q, out, part, stream);
+    return sh.block == 128 ? launch_waves<KIND, 64, 4>(tab, n_units, sh, cache, Q, out, part, stream)
+                           : launch_waves<KIND, 64, 8>(tab, n_units, sh, cache, Q, out, part, stream);
   }
-  return sh.block == 128 ? launch_nb<KIND, 128, 1>(tab, n_units, sh, cache, Q, out, part, stream)
-                         : launch_nb<KIND, 128, 2>(tab, n_units, sh, cache, Q, out, part, stream);
+  return sh.block == 128 ? launch_waves<KIND, 128, 4>(tab, n_units, sh, cache, Q, out, part, stream)
+                         : launch_waves<KIND, 128, 8>(tab, n_units, sh, cache, Q, out, part, stream);
 }
 
 }  // namespace
