@@ -13,8 +13,9 @@ constexpr uint32_t kNanScale = 255;
 // Scales are 2^-125 to 2^125: what they make of the codes is neither subnormal nor beyond the largest number.
 constexpr int kLeastScale = 127 - 125, kMostScale = 127 + 125;
 
-// The float that multiplies the codes of a block with scale byte s (255: a NaN).
-__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == kNanScale ? 0x7fffffffu : s << 23); }
+// What two_of takes for a block with scale byte s: the conversion looks at the float's exponent alone, as a scale byte, so that
+// 255 (an infinity) makes NaNs of all codes.
+__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s << 23); }
 
 // The two values of byte B of `codes`, as packed bf16 (exact).
 template <int B>

@@ -66,7 +66,12 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&s)[N]) {
 }
 
 // What a wavefront reads of a tile of 32 rows.  Lane l of the wavefront is column / row c = l % 16 of lane group g = l / 16;
-// key rows: 16 h + c (h = 0, 1), value rows: i < 4: 4 g + i, else 12 + 4 g + i.
+// key rows: 16 h + c (h = 0, 1), value rows: i < 4: 4 g + i, else 12 + 4 g + i.  A tile that its range's end cuts is read row by
+// row (rows past the end repeat the last one), any other from one address per lane.
+__device__ __forceinline__ int value_row(int g, int i) { return (i < 4 ? 0 : 12) + 4 * g + i; }
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+
 template <CacheKind KIND, int D> struct Rows;
 
 template <int D>
@@ -80,17 +85,27 @@ struct Rows<CacheKind::kBf16, D> {
   u32x4 k[2][kSteps];
   vpiece v[8];
   static __device__ __forceinline__ int channel(int s, int g) { return 32 * s + 8 * g; }
-  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int h, uint32_t row, int g) {
-    const char* base = (const char*)cache.k + row0 * (2 * D);
+  // t0: the tile's first row within the unit, last: its last row within the tile
+  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int t0, int last, int c, int g) {
+    const char* base = (const char*)cache.k + (row0 + t0) * (2 * D);
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) k[h][s] = at<u32x4>(base, row * (2 * D) + 16 * g + 64 * s);
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t row = last >= kTile - 1 ? 16 * h + c : min(16 * h + c, last);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) k[h][s] = at<u32x4>(base, row * (2 * D) + 16 * g + 64 * s);
+    }
   }
-  __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
-    v[i] = at<vpiece>((const char*)cache.v + row0 * (2 * D), row * (2 * D) + c * (D / 8));
+  __device__ __forceinline__ void load_values(const Cache& cache, size_t row0, int t0, int last, int c, int g) {
+    const char* base = (const char*)cache.v + (row0 + t0) * (2 * D);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t row = last >= kTile - 1 ? value_row(g, i) : min(value_row(g, i), last);
+      v[i] = at<vpiece>(base, row * (2 * D) + c * (D / 8));
+    }
   }
   __device__ __forceinline__ bf16x8 key(int h, int s) const { return __builtin_bit_cast(bf16x8, k[h][s]); }
   // channels 2 W, 2 W + 1 of the lane's
-  template <int W> __device__ __forceinline__ uint32_t value(int i) const { return v[i][W]; }
+  template <int W> __device__ __forceinline__ uint32_t value(int i, int) const { return v[i][W]; }
 };
 
 template <int D, bool F32>
@@ -105,22 +120,58 @@ struct PackedRows {
   kpiece k[2];
   uint8_t ks[2];
   vpiece v[8];
-  uint8_t vs[8];
+  uint32_t vs[D == 128 ? 8 : 4];           // the value rows' scales, all of a row's beside each other
   static __device__ __forceinline__ int channel(int s, int g) { return (D / 4) * g + 8 * s; }
-  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int h, uint32_t row, int g) {
-    k[h] = at<kpiece>((const char*)cache.k + row0 * (D / 2), row * (D / 2) + g * (D / 8));
-    ks[h] = at<uint8_t>((const char*)cache.ks + row0 * (D / 32), row * (D / 32) + g * (D / 4) / 32);
+  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int t0, int last, int c, int g) {
+    const char* base = (const char*)cache.k + (row0 + t0) * (D / 2);
+    const char* scales = (const char*)cache.ks + (row0 + t0) * (D / 32);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t row = last >= kTile - 1 ? 16 * h + c : min(16 * h + c, last);
+      k[h] = at<kpiece>(base, row * (D / 2) + g * (D / 8));
+      ks[h] = at<uint8_t>(scales, row * (D / 32) + g * (D / 4) / 32);
+    }
   }
-  __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
-    v[i] = at<vpiece>((const char*)cache.v + row0 * (D / 2), row * (D / 2) + c * (D / 32));
-    vs[i] = at<uint8_t>((const char*)cache.vs + row0 * (D / 32), row * (D / 32) + c * CPL / 32);
+  __device__ __forceinline__ void load_values(const Cache& cache, size_t row0, int t0, int last, int c, int g) {
+    const char* base = (const char*)cache.v + (row0 + t0) * (D / 2);
+    const char* scales = (const char*)cache.vs + (row0 + t0) * (D / 32);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t row = last >= kTile - 1 ? value_row(g, i) : min(value_row(g, i), last);
+      v[i] = at<vpiece>(base, row * (D / 2) + c * (D / 32));
+    }
+    if (last >= kTile - 1) {                 // four rows' scales lie together
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (D == 128) {
+          const u32x4_at4 x = at<u32x4_at4>(scales, (16 * h + 4 * g) * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vs[4 * h + i] = x[i];
+        } else {
+          const u32x2_at2 x = at<u32x2_at2>(scales, (16 * h + 4 * g) * 2);
+          vs[2 * h] = x[0];
+          vs[2 * h + 1] = x[1];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t row = min(value_row(g, i), last);
+        if constexpr (D == 128) vs[i] = at<uint32_t>(scales, row * 4);
+        else if (i % 2 == 0) vs[i / 2] = at<uint16_t>(scales, row * 2);
+        else vs[i / 2] |= (uint32_t)at<uint16_t>(scales, row * 2) << 16;
+      }
+    }
   }
   __device__ __forceinline__ bf16x8 key(int h, int s) const {
     const float sc = scale_of(ks[h]);
     const u32x4 w = {two_of<0>(k[h][s], sc), two_of<1>(k[h][s], sc), two_of<2>(k[h][s], sc), two_of<3>(k[h][s], sc)};
     return __builtin_bit_cast(bf16x8, w);
   }
-  template <int W> __device__ __forceinline__ uint32_t value(int i) const { return two_of<W>(v[i], scale_of(vs[i])); }
+  template <int W> __device__ __forceinline__ uint32_t value(int i, int c) const {
+    const uint32_t s = D == 128 ? vs[i] >> (c / 4 * 8) : vs[i / 2] >> (c / 8 * 8 + i % 2 * 16);
+    return two_of<W>(v[i], scale_of(s & 255u));
+  }
 };
 template <int D> struct Rows<CacheKind::kPackedBf16, D> : PackedRows<D, false> {};
 template <int D> struct Rows<CacheKind::kPackedF32, D> : PackedRows<D, true> {};
@@ -134,15 +185,23 @@ struct Rows<CacheKind::kF32, D> {
   f32x4 k[2][kSteps];
   f32x4 v[8][D / 64];
   static __device__ __forceinline__ int channel(int s, int g) { return 16 * s + 4 * g; }
-  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int h, uint32_t row, int g) {
-    const char* base = (const char*)cache.k + row0 * (4 * D);
+  __device__ __forceinline__ void load_keys(const Cache& cache, size_t row0, int t0, int last, int c, int g) {
+    const char* base = (const char*)cache.k + (row0 + t0) * (4 * D);
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) k[h][s] = at<f32x4>(base, row * (4 * D) + 16 * g + 64 * s);
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t row = last >= kTile - 1 ? 16 * h + c : min(16 * h + c, last);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) k[h][s] = at<f32x4>(base, row * (4 * D) + 16 * g + 64 * s);
+    }
   }
-  __device__ __forceinline__ void load_value(const Cache& cache, size_t row0, int i, uint32_t row, int c) {
-    const char* base = (const char*)cache.v + row0 * (4 * D);
+  __device__ __forceinline__ void load_values(const Cache& cache, size_t row0, int t0, int last, int c, int g) {
+    const char* base = (const char*)cache.v + (row0 + t0) * (4 * D);
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) v[i][e] = at<f32x4>(base, row * (4 * D) + 16 * c + 256 * e);
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t row = last >= kTile - 1 ? value_row(g, i) : min(value_row(g, i), last);
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) v[i][e] = at<f32x4>(base, row * (4 * D) + 16 * c + 256 * e);
+    }
   }
 };
 
@@ -188,8 +247,14 @@ __device__ __forceinline__ void store_two(T* at, float a, float b) {
   else *(uint32_t*)at = cvt_pk_bf16(a, b);
 }
 
-template <CacheKind KIND, int D, int NQ, typename Tab>
-__global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void window_rows_kernel(
+// Wavefronts per SIMD that the registers are allotted for: the operands of a tile and of the queries, and the accumulators.
+template <CacheKind KIND, int D, int NQ>
+constexpr int waves_per_simd() {
+  return KIND == CacheKind::kF32 && D == 128 ? (NQ == 1 ? 2 : 1) : NQ == 1 ? 3 : NQ == 2 ? 2 : 1;
+}
+
+template <CacheKind KIND, int D, int NQ, bool COUNTS, typename Tab>
+__global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void window_rows_kernel(
     const Tab tab, const WindowShape sh, const Cache cache, const void* __restrict__ Q, void* __restrict__ out,
     float* __restrict__ part) {
   typedef Rows<KIND, D> L;
@@ -230,7 +295,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void windo
     Queries<L, D, NQ> qs;
     qs.load((const Io*)Q, sh, un.index, row0, c, g);
     L rows;
-    float cnt[8];
+    uint32_t cnt[8];
     // tile j: its first row, and the end of the range of rows that it is in (rows past it repeat the last one)
     auto start_of = [&](int t) { return t < re.sink_tiles ? t * kTile : re.first + (t - re.sink_tiles) * kTile; };
     auto end_of = [&](int t) { return t < re.sink_tiles ? re.sink_end : re.end; };
@@ -239,18 +304,26 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void windo
       return t0 + kTile <= end && t0 + kTile - 1 <= re.pos_min &&
              (sh.span == 0 || t0 > re.pos_max - sh.span || t0 + kTile <= sh.sinks);
     };
-    auto load_keys = [&](int t) {
-      const int t0 = start_of(t), last = end_of(t) - 1;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) rows.load_keys(cache, un.in_row, h, min(t0 + 16 * h + c, last), g);
+    auto load_keys = [&](int t) __attribute__((always_inline)) {
+      const int t0 = start_of(t);
+      rows.load_keys(cache, un.in_row, t0, end_of(t) - 1 - t0, c, g);
     };
-    auto load_values = [&](int t) {
-      const int t0 = start_of(t), last = end_of(t) - 1;
+    auto load_values = [&](int t) __attribute__((always_inline)) {
+      const int t0 = start_of(t), last = end_of(t) - 1 - t0;
+      rows.load_values(cache, un.in_row, t0, last, c, g);
+      if constexpr (COUNTS) {
+        const char* base = (const char*)(cache.counts + un.in_row + t0);
+        if (last >= kTile - 1) {               // four rows' cardinalities lie together
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = min(t0 + (i < 4 ? 0 : 12) + 4 * g + i, last);
-        rows.load_value(cache, un.in_row, i, row, c);
-        cnt[i] = cache.counts ? (float)cache.counts[un.in_row + row] : 1.f;
+          for (int h = 0; h < 2; ++h) {
+            const u32x4_at4 x = at<u32x4_at4>(base, (16 * h + 4 * g) * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cnt[4 * h + i] = x[i];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) cnt[i] = at<uint32_t>(base, min(value_row(g, i), last) * 4);
+        }
       }
     };
     const int j0 = j;
@@ -293,12 +366,20 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void windo
       for (int n = 0; n < NQ; ++n) {
         float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int t = t0 + (i < 4 ? 0 : 12) + 4 * g + i;
-          const float x = s[n][i / 4][i % 4] * sh.scale_log2;
-          p[n][i] = whole || (t < end && sees(sh, pos[n], t)) ? x : -INFINITY;
-          top = fmaxf(top, p[n][i]);
+        for (int i = 0; i < 8; ++i) p[n][i] = s[n][i / 4][i % 4] * sh.scale_log2;
+        if (!whole) {
+          // the lane's rows are x = i or 12 + i plus this: limits that x is compared with
+          const int base = t0 + 4 * g, before_sinks = sh.sinks - base;
+          const int last = min(pos[n], end - 1) - base;
+          const int hidden = sh.span > 0 ? pos[n] - sh.span - base : -1 - base;  // rows up to here are seen as sinks only
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int x = value_row(0, i);
+            p[n][i] = (x <= last) & ((x > hidden) | (x < before_sinks)) ? p[n][i] : -INFINITY;
+          }
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, p[n][i]);
         if (__ballot(top > m[n] + kSlack) != 0) {            // rare after the first tiles
           top = fmaxf(top, __shfl_xor(top, 16, kWave));      // the four lane groups feed the same columns of O^T
           top = fmaxf(top, __shfl_xor(top, 32, kWave));
@@ -314,7 +395,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void windo
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           p[n][i] = __builtin_amdgcn_exp2f(p[n][i] - ref);
-          sum = fmaf(cnt[i], p[n][i], sum);                  // c copies of the slot in the denominator
+          if constexpr (COUNTS) sum = fmaf((float)(int)cnt[i], p[n][i], sum);   // c copies of the slot in the denominator
+          else sum += p[n][i];
         }
         l[n] += sum;
       }
@@ -325,7 +407,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 3 : NQ == 2 ? 2 : 1) void windo
           constexpr int W2 = decltype(w)::value;
 #pragma unroll
           for (int i = 0; i < 8; i += 2) {
-            const uint32_t a = rows.template value<W2>(i), b = rows.template value<W2>(i + 1);
+            const uint32_t a = rows.template value<W2>(i, c), b = rows.template value<W2>(i + 1, c);
             vt[2 * W2][i / 2] = __builtin_amdgcn_perm(b, a, 0x05040100u);
             vt[2 * W2 + 1][i / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
           }
@@ -521,8 +603,14 @@ hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const
                        float* part, hipStream_t stream) {
   const dim3 grid((unsigned)((long long)n_units * sh.n_blocks * sh.n_parts));
   auto go = [&](auto nq) {
-    hipLaunchKernelGGL((window_rows_kernel<KIND, D, decltype(nq)::value, Tab>), grid, dim3(kThreads), 0, stream, tab, sh,
-                       cache, Q, out, part);
+    constexpr int NQ = decltype(nq)::value;
+    if (cache.counts) {
+      hipLaunchKernelGGL((window_rows_kernel<KIND, D, NQ, true, Tab>), grid, dim3(kThreads), 0, stream, tab, sh, cache, Q, out,
+                         part);
+    } else {
+      hipLaunchKernelGGL((window_rows_kernel<KIND, D, NQ, false, Tab>), grid, dim3(kThreads), 0, stream, tab, sh, cache, Q, out,
+                         part);
+    }
   };
   if (sh.block == 16) go(std::integral_constant<int, 1>{});
   else if (sh.block == 32) go(std::integral_constant<int, 2>{});
