@@ -65,19 +65,31 @@ long long tiles_bound(const WindowShape& sh, int len, int tile) {
   return tiles(std::min<long long>(len, sh.span + positions - 1)) + tiles(std::min(sh.sinks, len));
 }
 
-// How the rows that a block sees are cut into pieces: workgroups enough for the chip, and pieces long enough for what a
-// workgroup does once.
-void cut_into_parts(const kvs_problem* p, bool wide, WindowShape& sh) {
-  const long long wanted = wide ? 256 : 1024, least = wide ? 4 : 8;
-  long long total = 0, most = 1;
-  for (int u = 0; u < p->n_units; ++u) {
-    const long long t = tiles_bound(sh, p->len[u], wide ? kWideTile : kWindowTile);
-    total += t * sh.n_blocks;
-    most = std::max(most, t);
+// How the rows that a block sees are cut into pieces: the longest that make no more workgroups than run at once, `at_once`
+// (all of a call's workgroups take as long, and what one does for its piece, a partial result written and read again, is done
+// as rarely as possible).
+void cut_into_parts(const kvs_problem* p, int tile, long long at_once, WindowShape& sh) {
+  constexpr long long kLeastTiles = 4;           // a tile for each wavefront of a workgroup, or as much work as that
+  long long most = 1;
+  for (int u = 0; u < p->n_units; ++u) most = std::max(most, tiles_bound(sh, p->len[u], tile));
+  auto workgroups = [&](long long per) {
+    long long n = 0, parts = 0;
+    for (int u = 0; u < p->n_units; ++u) {
+      if (u == 0 || p->len[u] != p->len[u - 1]) parts = std::max(1ll, (tiles_bound(sh, p->len[u], tile) + per - 1) / per);
+      n += parts * sh.n_blocks;
+    }
+    return n;
+  };
+  long long per = std::max(kLeastTiles, (most + kMaxParts - 1) / kMaxParts);
+  if (workgroups(per) > at_once) {
+    long long fits = std::max(per, most);        // (whole reaches, whether or not they fit)
+    while (fits - per > 1) {
+      const long long mid = (per + fits) / 2;
+      if (workgroups(mid) > at_once) per = mid;
+      else fits = mid;
+    }
+    per = fits;
   }
-  long long per = std::max((total + wanted - 1) / wanted, least);
-  if (wide && (long long)p->n_units * sh.n_blocks >= wanted) per = most;
-  per = std::max(per, (most + kMaxParts - 1) / kMaxParts);
   sh.part_tiles = (int)per;
   sh.n_parts = (int)((most + per - 1) / per);
 }
@@ -98,10 +110,18 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
   sh.sinks = std::min(p->n_sink, KVS_MAX_LEN);
   const double scale = p->scale == 0.f ? 1.0 / std::sqrt((double)p->head_dim) : (double)p->scale;
   sh.scale_log2 = (float)(scale * 1.4426950408889634);
-  plan->wide = *elt == 2 && !packed && sh.R > 64;
+  // From 33 bf16 rows of 128 channels on tiles go through LDS, from 65 rows of 64 channels (64 caches of 8224 rows: 64 query rows
+  // of 128 channels 76.7 us against 102.2, plain, and 75.4 against 84.9 in 4 bits, of 64 channels 54.7 against 49.6; 32 rows
+  // of 128 channels 71.7 against 59.8; 128 rows 84 against 164).
+  plan->wide = *elt == 2 && sh.R > (sh.D == 128 ? 32 : 64);
   sh.block = plan->wide ? (sh.R <= 128 ? 128 : 256) : sh.R <= 16 ? 16 : sh.R <= 32 ? 32 : 64;
   sh.n_blocks = (sh.R + sh.block - 1) / sh.block;
-  cut_into_parts(p, plan->wide, sh);
+  // Workgroups that run at once.  One per compute unit keeps memory busy with plain rows (one token on 64 caches of 8224 rows:
+  // 54.7 us with 256 workgroups, 57.2 with 512, 58.2 with 768).  Of those that read rows in 4 bits as many as fit the registers
+  // (22 and 65 tiles a piece are 768 and 256: 64 channels 18.9 and 26.0 us; 16 query rows 27.4 and 37.8).
+  const int per_unit = !packed ? 1 : sh.block == 16 ? 3 : sh.block == 32 || sh.block == 128 ? 2 : 1;
+  const long long at_once = 256ll * per_unit;
+  cut_into_parts(p, plan->wide ? kWideTile : kWindowTile, at_once, sh);
   plan->equal = true;
   for (int u = 1; u < p->n_units; ++u) {
     plan->equal = plan->equal && p->len[u] == p->len[0] && p->in_row[u] - p->in_row[u - 1] == p->in_row[1] - p->in_row[0];
@@ -110,6 +130,19 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
     plan->part_bytes = align_up((size_t)p->n_units * sh.R * sh.n_parts * (sh.D + 2) * sizeof(float));
   }
   if (!plan->equal && p->n_units > kInlineUnits) plan->table_bytes = align_up((size_t)p->n_units * sizeof(CacheUnit));
+  return KVS_OK;
+}
+
+// One size for both forms.
+kvs_status window_workspace(const kvs_problem* p, int32_t span, size_t* bytes) {
+  *bytes = 0;
+  for (const bool packed : {false, true}) {
+    WindowPlan plan;
+    int elt = 0;
+    const kvs_status st = make_window_plan(p, span, packed, &plan, &elt);
+    if (st != KVS_OK) return st;
+    *bytes = std::max(*bytes, plan.bytes());
+  }
   return KVS_OK;
 }
 
@@ -128,7 +161,9 @@ kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, con
   kvs_status st = make_window_plan(p, span, packed, &plan, &elt);
   if (st != KVS_OK) return st;
   const WindowShape& sh = plan.sh;
-  if (plan.bytes() > 0 && (ws == nullptr || ((uintptr_t)ws % kAlign) != 0 || ws_bytes < plan.bytes())) return KVS_ERR_WORKSPACE;
+  size_t need = 0;
+  if ((st = window_workspace(p, span, &need)) != KVS_OK) return st;
+  if (need > 0 && (ws == nullptr || ((uintptr_t)ws % kAlign) != 0 || ws_bytes < need)) return KVS_ERR_WORKSPACE;
   const size_t rows = rows_to(p, p->in_row), qo = (size_t)p->n_units * sh.R * sh.D * elt;
   const size_t row_bytes = packed ? (size_t)sh.D / 2 : (size_t)sh.D * elt;
   Buffers b;
@@ -141,7 +176,7 @@ kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, con
   }
   if (cache.counts) b.add(cache.counts, rows * 4, false);
   b.add(out, qo, true);
-  b.add(ws, plan.bytes(), true);
+  b.add(ws, need, true);
   if ((st = check_ranges(b.r, b.n)) != KVS_OK) return st;
 
   const hipStream_t s = (hipStream_t)hip_stream;
@@ -260,16 +295,10 @@ extern "C" {
 
 kvs_status kvs_window_attention_workspace_size(const kvs_problem* p, int32_t span, size_t* bytes) {
   if (bytes == nullptr) return KVS_ERR_INVALID_ARG;
-  size_t most = 0;                             // (one size for both forms)
-  for (const bool packed : {false, true}) {
-    WindowPlan plan;
-    int elt = 0;
-    const kvs_status st = make_window_plan(p, span, packed, &plan, &elt);
-    if (st != KVS_OK) return st;
-    most = std::max(most, plan.bytes());
-  }
-  *bytes = most;
-  return KVS_OK;
+  size_t need = 0;
+  const kvs_status st = window_workspace(p, span, &need);
+  if (st == KVS_OK) *bytes = need;
+  return st;
 }
 
 kvs_status kvs_window_attention(const kvs_problem* p, int32_t span, const void* Q, const void* K, const void* V,

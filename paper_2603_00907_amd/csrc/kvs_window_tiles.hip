@@ -1,4 +1,5 @@
-// The attention of kvs_window_rows.hip for blocks of many query rows, bf16: a prompt, or a chunk of new tokens on a cache.
+// The attention of kvs_window_rows.hip for blocks of many query rows, bf16 ones: a prompt, or a chunk of new tokens on a cache.
+// Rows in 4 bits become bf16 on their way into LDS.
 //
 // What bounds it is the matrix cores (4 D operations per query and row against 4 D bytes per row of the cache), so tiles of 64
 // cache rows go through LDS, once for the 128 NB query rows of a workgroup, and every operand read feeds NB products.
@@ -51,8 +52,51 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 x, bool& odd) {
 
 __device__ __forceinline__ float of_both_halves_max(float x) { return fmaxf(x, __shfl_xor(x, 32, kWave)); }
 
+// A thread's pieces of a tile of K or V on their way from memory: piece `p` (eight channels) of every (THREADS * 8 / D)-th row,
+// from row `srow` of the tile on.  Rows past the range's end, row `last` of the tile, repeat it.
+template <CacheKind KIND, int D, int THREADS>
+struct Staged {
+  static constexpr int kStep = THREADS * 8 / D, kPer = kTile / kStep;
+  u32x4 r[kPer];
+  __device__ __forceinline__ void request(const void* rows, const uint8_t*, long long first, int last, int srow, int p) {
+    const char* base = (const char*)rows + (size_t)first * (2 * D);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t row = last >= kTile - 1 ? srow + i * kStep : min(srow + i * kStep, last);
+      r[i] = *(const u32x4*)(base + (uint32_t)(row * (2 * D) + 16 * p));
+    }
+  }
+  __device__ __forceinline__ u32x4 piece(int i) const { return r[i]; }
+};
+template <int D, int THREADS>
+struct Staged<CacheKind::kPackedBf16, D, THREADS> {
+  static constexpr int kStep = THREADS * 8 / D, kPer = kTile / kStep;
+  uint32_t r[kPer];
+  uint8_t s[kPer];
+  __device__ __forceinline__ void request(const void* rows, const uint8_t* scales, long long first, int last, int srow, int p) {
+    const char* base = (const char*)rows + (size_t)first * (D / 2);
+    const uint8_t* sbase = scales + (size_t)first * (D / 32);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t row = last >= kTile - 1 ? srow + i * kStep : min(srow + i * kStep, last);
+      r[i] = *(const uint32_t*)(base + (uint32_t)(row * (D / 2) + 4 * p));
+      s[i] = sbase[row * (D / 32) + p / 4];
+    }
+  }
+  __device__ __forceinline__ u32x4 piece(int i) const {
+    const float sc = fp4::scale_of(s[i]);
+    return u32x4{fp4::two_of<0>(r[i], sc), fp4::two_of<1>(r[i], sc), fp4::two_of<2>(r[i], sc), fp4::two_of<3>(r[i], sc)};
+  }
+};
+
+// Wavefronts per SIMD that the registers are allotted for.  With four wavefronts per workgroup two of those share a compute unit
+// where the pieces on their way are rows in 4 bits (8 caches of 131072 rows, 64 query rows: 86 us, one workgroup 126); those of
+// plain rows would have to be spilled (64 of 8224: 84 us, one workgroup 77).
+template <CacheKind KIND, int WAVES>
+constexpr int waves_per_simd() { return WAVES == 8 || KIND == CacheKind::kPackedBf16 ? 2 : 1; }
+
 template <CacheKind KIND, int D, int WAVES, bool COUNTS, typename Tab>
-__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 1) void window_tiles_kernel(
+__global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, WAVES>())) void window_tiles_kernel(
     const Tab tab, const WindowShape sh, const Cache cache, int n_units, const uint16_t* __restrict__ Q,
     uint16_t* __restrict__ out, float* __restrict__ part) {
   constexpr int kThreads = WAVES * kWave;
@@ -97,47 +141,38 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 1) void window_tile
     const uint16_t* src = Q + query_row(sh, un.index, min(row, sh.R - 1)) * D + 8 * half;
 #pragma unroll
     for (int k = 0; k < KS; ++k) q[k] = *(const bf16x8*)(src + 16 * k);
-    const char* kbase = (const char*)cache.k + (size_t)un.in_row * (2 * D);
-    const char* vbase = (const char*)cache.v + (size_t)un.in_row * (2 * D);
-    const int32_t* counts = COUNTS ? cache.counts + un.in_row : nullptr;
     // A tile travels through registers: requested when a tile is begun, written to LDS when that one is nearly done.
-    // (Rows past the range's end repeat the last one.)
     const int srow = tid / PPR, spiece = tid % PPR;
-    u32x4 rk[PER], rv[PER];
+    Staged<KIND, D, kThreads> rk, rv;
     float rc = 1.f;
-    const uint32_t soffset = srow * (2 * D) + 16 * spiece;
-    auto request = [&](const char* base, int t, u32x4 (&r)[PER]) __attribute__((always_inline)) {
-      const int t0 = start_of(t), last = end_of(t) - 1 - t0;
-      const char* first = base + (uint32_t)t0 * (2 * D);
-      if (last >= kTile - 1) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) r[i] = *(const u32x4*)(first + i * (kThreads / PPR) * (2 * D) + soffset);
-      } else {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          r[i] = *(const u32x4*)(first + (uint32_t)(min(srow + i * (kThreads / PPR), last) * (2 * D) + 16 * spiece));
-      }
+    auto request = [&](auto& r, const void* rows, const uint8_t* scales, int t) __attribute__((always_inline)) {
+      const int t0 = start_of(t);
+      r.request(rows, scales, un.in_row + t0, end_of(t) - 1 - t0, srow, spiece);
     };
+    auto request_keys = [&](int t) __attribute__((always_inline)) { request(rk, cache.k, cache.ks, t); };
     auto request_values = [&](int t) __attribute__((always_inline)) {
-      request(vbase, t, rv);
-      if (COUNTS && tid < kTile) rc = (float)counts[start_of(t) + min(tid, end_of(t) - 1 - start_of(t))];
+      request(rv, cache.v, cache.vs, t);
+      if (COUNTS && tid < kTile) rc = (float)cache.counts[un.in_row + start_of(t) + min(tid, end_of(t) - 1 - start_of(t))];
     };
     auto store_keys = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int row = srow + i * (kThreads / PPR);
-        sm_k[b][row * PPR + key_slot<D>(row, spiece)] = rk[i];
+        sm_k[b][row * PPR + key_slot<D>(row, spiece)] = rk.piece(i);
       }
     };
     auto store_values = [&](int t, int b) __attribute__((always_inline)) {
+      u32x4 x[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) x[i] = rv.piece(i);
       if (!seen_whole(start_of(t), end_of(t), re.pos_min, re.pos_max)) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) rv[i] = finite_only(rv[i], odd);
+        for (int i = 0; i < PER; ++i) x[i] = finite_only(x[i], odd);
       }
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int row = srow + i * (kThreads / PPR);
-        sm_v[b][row * PPR + value_slot<D>(row, spiece)] = rv[i];
+        sm_v[b][row * PPR + value_slot<D>(row, spiece)] = x[i];
       }
       if (COUNTS && tid < kTile) {
         const uint32_t hi = cvt_pk_bf16(rc, 0.f);
@@ -250,10 +285,10 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 1) void window_tile
       }
     };
 
-    request(kbase, j0, rk);
+    request_keys(j0);
     request_values(j0);
     store_keys(0);
-    if (j0 + 1 < j1) request(kbase, j0 + 1, rk);
+    if (j0 + 1 < j1) request_keys(j0 + 1);
     store_values(j0, 0);
     if (j0 + 1 < j1) store_keys(1);
     __syncthreads();
@@ -267,7 +302,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 1) void window_tile
     auto tile = [&](int j, auto buffer_c) __attribute__((always_inline)) {
       constexpr int B = decltype(buffer_c)::value;
       if (j + 1 < j1) request_values(j + 1);
-      if (j + 2 < j1) request(kbase, j + 2, rk);
+      if (j + 2 < j1) request_keys(j + 2);
       step(std::integral_constant<int, 0>{}, buffer_c, j, s0, s1);
       step(std::integral_constant<int, 1>{}, buffer_c, j, s1, s0);
       if (j + 1 < j1) {
@@ -361,9 +396,13 @@ hipError_t launch_sized(const Tab& tab, int n_units, const WindowShape& sh, cons
 }  // namespace
 
 hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                               CacheKind, const Cache& cache, const void* Q, void* out, float* part, hipStream_t stream) {
-  const hipError_t e = equal ? launch_sized<CacheKind::kBf16>(*equal, n_units, sh, cache, Q, out, part, stream)
-                             : launch_sized<CacheKind::kBf16>(*listed, n_units, sh, cache, Q, out, part, stream);
+                               CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
+                               hipStream_t stream) {
+  auto go = [&](const auto& tab) {
+    return kind == CacheKind::kBf16 ? launch_sized<CacheKind::kBf16>(tab, n_units, sh, cache, Q, out, part, stream)
+                                    : launch_sized<CacheKind::kPackedBf16>(tab, n_units, sh, cache, Q, out, part, stream);
+  };
+  const hipError_t e = equal ? go(*equal) : go(*listed);
   if (e != hipSuccess || sh.n_parts == 1) return e;
   return launch_window_reduce(equal, listed, n_units, sh, false, kTile, part, out, stream);
 }

@@ -37,8 +37,8 @@ hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, Cac
   return hipSuccess;
 }
 
-hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                              CacheKind, const Cache&, const void*, void*, float* part, hipStream_t) {
+template <int TILE>
+hipError_t attended(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh, float* part) {
   CHECK((equal != nullptr) != (listed != nullptr));
   CHECK(n_units > 0 && (listed == nullptr || listed->ext != nullptr || n_units <= kInlineUnits));
   CHECK((long long)n_units * sh.n_blocks * sh.n_parts < 1ll << 24);
@@ -52,10 +52,10 @@ hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed
     g_done.push_back(un.index);
     CHECK(un.len == g_problem->len[un.index] && un.in_row == g_problem->in_row[un.index]);
     for (int b = 0; b < sh.n_blocks; b += 1 + sh.n_blocks / 20) {
-      const Reach r = reach_of<kWindowTile>(sh, un.len, b);
+      const Reach r = reach_of<TILE>(sh, un.len, b);
       CHECK(parts_of(r.tiles, sh.part_tiles) <= sh.n_parts);
       CHECK(0 <= r.sink_end && r.sink_end <= r.first && r.first <= r.end && r.end <= un.len);
-      CHECK(r.sink_tiles * kWindowTile >= r.sink_end && (r.tiles - r.sink_tiles) * kWindowTile >= r.end - r.first);
+      CHECK(r.sink_tiles * TILE >= r.sink_end && (r.tiles - r.sink_tiles) * TILE >= r.end - r.first);
     }
     if (sh.n_parts > 1) {
       const size_t last = (((size_t)un.index * sh.R + sh.R - 1) * sh.n_parts + sh.n_parts - 1) * (sh.D + 2) + sh.D + 2;
@@ -64,6 +64,17 @@ hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed
     }
   }
   return hipSuccess;
+}
+hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
+                              CacheKind, const Cache&, const void*, void*, float* part, hipStream_t) {
+  CHECK(sh.block == 16 || sh.block == 32 || sh.block == 64);
+  return attended<kWindowTile>(equal, listed, n_units, sh, part);
+}
+hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
+                               CacheKind kind, const Cache&, const void*, void*, float* part, hipStream_t) {
+  CHECK(sh.block == 128 || sh.block == 256);
+  CHECK(kind == CacheKind::kBf16 || kind == CacheKind::kPackedBf16);
+  return attended<kWideTile>(equal, listed, n_units, sh, part);
 }
 
 namespace {
