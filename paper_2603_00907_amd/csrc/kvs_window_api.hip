@@ -110,16 +110,25 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
   sh.sinks = std::min(p->n_sink, KVS_MAX_LEN);
   const double scale = p->scale == 0.f ? 1.0 / std::sqrt((double)p->head_dim) : (double)p->scale;
   sh.scale_log2 = (float)(scale * 1.4426950408889634);
-  // From 33 bf16 rows of 128 channels on tiles go through LDS, from 65 rows of 64 channels (64 caches of 8224 rows: 64 query rows
-  // of 128 channels 76.7 us against 102.2, plain, and 75.4 against 84.9 in 4 bits, of 64 channels 54.7 against 49.6; 32 rows
-  // of 128 channels 71.7 against 59.8; 128 rows 84 against 164).
-  plan->wide = *elt == 2 && sh.R > (sh.D == 128 ? 32 : 64);
-  sh.block = plan->wide ? (sh.R <= 128 ? 128 : 256) : sh.R <= 16 ? 16 : sh.R <= 32 ? 32 : 64;
+  // From 33 bf16 query rows on tiles go through LDS (64 caches of 8224 rows: 64 query rows 76.7 us against 102, in 4 bits 55 against
+  // 85; 32 rows 71.7 against 59.8).
+  plan->wide = *elt == 2 && sh.R > 32;
+  // Blocks of 32 query rows below that and with fp32 outputs, whose rows from 17 on would otherwise read the cache once per 16 (fp32,
+  // 64 caches of 8192 rows, 64 query rows: 178 us against 229; blocks of 64 leave one wavefront per SIMD, 240).  Blocks of 16
+  // where an fp32 cache stays in the memory-side cache, since the matrix cores then bound it and one wavefront more hides
+  // what the others wait for (16 of 4096, 256 rows: 91 against 102).
+  bool small = sh.R <= 16;
+  if (*elt == 4 && !packed) {
+    long long bytes = 0;
+    for (int u = 0; u < p->n_units; ++u) bytes += 2ll * p->len[u] * sh.D * 4;
+    small = small || bytes <= kStreamBytes;
+  }
+  sh.block = plan->wide ? (sh.R <= 128 ? 128 : 256) : small ? 16 : 32;
   sh.n_blocks = (sh.R + sh.block - 1) / sh.block;
   // Workgroups that run at once.  One per compute unit keeps memory busy with plain rows (one token on 64 caches of 8224 rows:
   // 54.7 us with 256 workgroups, 57.2 with 512, 58.2 with 768).  Of those that read rows in 4 bits as many as fit the registers
-  // (22 and 65 tiles a piece are 768 and 256: 64 channels 18.9 and 26.0 us; 16 query rows 27.4 and 37.8).
-  const int per_unit = !packed ? 1 : sh.block == 16 ? 3 : sh.block == 32 || sh.block == 128 ? 2 : 1;
+  // (64 channels, pieces of 22 and 65 tiles: 768 workgroups 18.9 us, 256 26.0; 16 query rows of 128 channels 27.4 and 37.8).
+  const int per_unit = !packed ? 1 : sh.block == 16 ? 3 : sh.block == 256 ? 1 : 2;
   const long long at_once = 256ll * per_unit;
   cut_into_parts(p, plan->wide ? kWideTile : kWindowTile, at_once, sh);
   plan->equal = true;

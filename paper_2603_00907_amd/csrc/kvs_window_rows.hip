@@ -112,7 +112,8 @@ template <int D, bool F32>
 struct PackedRows {
   typedef std::conditional_t<F32, float, uint16_t> Io;
   static constexpr bool kMatrixF32 = false;
-  static constexpr int kQ = F32 ? 3 : 1, kP = F32 ? 3 : 2;
+  // (one number per weight: its error of 2^-9, of any sign, is far below that of the rows)
+  static constexpr int kQ = F32 ? 3 : 1, kP = F32 ? 3 : 1;
   static constexpr int kSteps = D / 32;
   static constexpr int CPL = D / 16;
   typedef uint32_t kpiece __attribute__((ext_vector_type(D / 32)));
@@ -169,8 +170,11 @@ struct PackedRows {
     return __builtin_bit_cast(bf16x8, w);
   }
   template <int W> __device__ __forceinline__ uint32_t value(int i, int c) const {
-    const uint32_t s = D == 128 ? vs[i] >> (c / 4 * 8) : vs[i / 2] >> (c / 8 * 8 + i % 2 * 16);
-    return two_of<W>(v[i], scale_of(s & 255u));
+    // byte c / 4 (D = 64: c / 8, of the upper half-word for an odd row) turned to where a float has its exponent, which is all
+    // that the conversion looks at
+    const uint32_t s = D == 128 ? vs[i] : vs[i / 2];
+    const uint32_t by = D == 128 ? c / 4 * 8 + 9 : c / 8 * 8 + i % 2 * 16 + 9;
+    return two_of<W>(v[i], __uint_as_float(__builtin_amdgcn_alignbit(s, s, by)));
   }
 };
 template <int D> struct Rows<CacheKind::kPackedBf16, D> : PackedRows<D, false> {};
@@ -250,7 +254,7 @@ __device__ __forceinline__ void store_two(T* at, float a, float b) {
 // Wavefronts per SIMD that the registers are allotted for: the operands of a tile and of the queries, and the accumulators.
 template <CacheKind KIND, int D, int NQ>
 constexpr int waves_per_simd() {
-  return KIND == CacheKind::kF32 && D == 128 ? (NQ == 1 ? 2 : 1) : NQ == 1 ? 3 : NQ == 2 ? 2 : 1;
+  return KIND == CacheKind::kF32 && D == 128 ? (NQ == 1 ? 2 : 1) : NQ == 1 && KIND != CacheKind::kBf16 ? 3 : 2;
 }
 
 template <CacheKind KIND, int D, int NQ, bool COUNTS, typename Tab>
@@ -366,7 +370,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
       for (int n = 0; n < NQ; ++n) {
         float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[n][i] = s[n][i / 4][i % 4] * sh.scale_log2;
+        for (int i = 0; i < 8; ++i) p[n][i] = s[n][i / 4][i % 4];
         if (!whole) {
           // the lane's rows are x = i or 12 + i plus this: limits that x is compared with
           const int base = t0 + 4 * g, before_sinks = sh.sinks - base;
@@ -379,7 +383,8 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, p[n][i]);
+        for (int i = 0; i < 8; i += 2) top = fmaxf(fmaxf(top, p[n][i]), p[n][i + 1]);
+        top *= sh.scale_log2;
         if (__ballot(top > m[n] + kSlack) != 0) {            // rare after the first tiles
           top = fmaxf(top, __shfl_xor(top, 16, kWave));      // the four lane groups feed the same columns of O^T
           top = fmaxf(top, __shfl_xor(top, 32, kWave));
@@ -394,7 +399,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[n][i] = __builtin_amdgcn_exp2f(p[n][i] - ref);
+          p[n][i] = __builtin_amdgcn_exp2f(fmaf(p[n][i], sh.scale_log2, -ref));
           if constexpr (COUNTS) sum = fmaf((float)(int)cnt[i], p[n][i], sum);   // c copies of the slot in the denominator
           else sum += p[n][i];
         }
@@ -613,8 +618,7 @@ hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const
     }
   };
   if (sh.block == 16) go(std::integral_constant<int, 1>{});
-  else if (sh.block == 32) go(std::integral_constant<int, 2>{});
-  else go(std::integral_constant<int, 4>{});
+  else go(std::integral_constant<int, 2>{});
   return hipGetLastError();
 }
 

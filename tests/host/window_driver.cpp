@@ -67,7 +67,7 @@ hipError_t attended(const EqualUnits* equal, const ListedUnits* listed, int n_un
 }
 hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
                               CacheKind, const Cache&, const void*, void*, float* part, hipStream_t) {
-  CHECK(sh.block == 16 || sh.block == 32 || sh.block == 64);
+  CHECK(sh.block == 16 || sh.block == 32);
   return attended<kWindowTile>(equal, listed, n_units, sh, part);
 }
 hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
