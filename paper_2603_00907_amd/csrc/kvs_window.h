@@ -58,6 +58,7 @@ struct WindowShape {
   int n_blocks;         // per unit
   int n_parts;          // pieces of the unit and block that has most of them
   int part_tiles;       // tiles per piece
+  int large;            // kvs_window_rows.hip: workgroups of all the wavefronts that a compute unit holds, and no pieces
 };
 
 // Query rows are taken in the order (window position, head), so that a block of them has few positions and its rows of the

@@ -32,9 +32,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = kWindowTile;
+constexpr int kReduceThreads = 256;
 
 // A piece of a unit's rows (at most 2^31 bytes of them): one scalar base, 32-bit offsets.
 template <typename T>
@@ -257,8 +256,8 @@ constexpr int waves_per_simd() {
   return KIND == CacheKind::kF32 && D == 128 ? (NQ == 1 ? 2 : 1) : NQ == 1 && KIND != CacheKind::kBf16 ? 3 : 2;
 }
 
-template <CacheKind KIND, int D, int NQ, bool COUNTS, typename Tab>
-__global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void window_rows_kernel(
+template <CacheKind KIND, int D, int NQ, int WAVES, bool COUNTS, typename Tab>
+__global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, NQ>())) void window_rows_kernel(
     const Tab tab, const WindowShape sh, const Cache cache, const void* __restrict__ Q, void* __restrict__ out,
     float* __restrict__ part) {
   typedef Rows<KIND, D> L;
@@ -266,7 +265,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
   constexpr bool F32 = L::kMatrixF32;
   constexpr int NJ = D / 16;                // accumulators of O^T per column block
   constexpr int ACCW = D + 4;               // numerators, maximum, denominator; rows stay 16-byte aligned
-  __shared__ __attribute__((aligned(16))) float sm_acc[kWaves][16][ACCW];
+  __shared__ __attribute__((aligned(16))) float sm_acc[WAVES][16][ACCW];
 
   const int id = blockIdx.x;
   const int piece = id % sh.n_parts, block = id / sh.n_parts % sh.n_blocks;
@@ -298,8 +297,6 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
   if (j < tile1) {
     Queries<L, D, NQ> qs;
     qs.load((const Io*)Q, sh, un.index, row0, c, g);
-    L rows;
-    uint32_t cnt[8];
     // tile j: its first row, and the end of the range of rows that it is in (rows past it repeat the last one)
     auto start_of = [&](int t) { return t < re.sink_tiles ? t * kTile : re.first + (t - re.sink_tiles) * kTile; };
     auto end_of = [&](int t) { return t < re.sink_tiles ? re.sink_end : re.end; };
@@ -308,6 +305,8 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
       return t0 + kTile <= end && t0 + kTile - 1 <= re.pos_min &&
              (sh.span == 0 || t0 > re.pos_max - sh.span || t0 + kTile <= sh.sinks);
     };
+    L rows;
+    uint32_t cnt[8];
     auto load_keys = [&](int t) __attribute__((always_inline)) {
       const int t0 = start_of(t);
       rows.load_keys(cache, un.in_row, t0, end_of(t) - 1 - t0, c, g);
@@ -336,7 +335,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
     load_values(j);
     while (true) {
       const int t0 = start_of(j), end = end_of(j);
-      const int next = j + kWaves;
+      const int next = j + WAVES;
       // S[t, q]: element v of half h is row 16 h + 4 g + v of the tile, query column c
       f32x4 s[NQ][2];
 #pragma unroll
@@ -476,7 +475,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
     }
     if (__ballot(odd) != 0) {
       // What is not finite makes the sums of the queries that see it what it is itself, whatever its weight.
-      for (j = j0; j < tile1; j += kWaves) {
+      for (j = j0; j < tile1; j += WAVES) {
         const int t0 = start_of(j), end = end_of(j);
         if (seen_whole(t0, end)) continue;
 #pragma unroll 1
@@ -515,15 +514,15 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
     }
     if (g == 0) { sm_acc[wave][c][D] = m[n]; sm_acc[wave][c][D + 1] = den; }
     __syncthreads();
-    for (int o = tid; o < 16 * D / 2; o += kThreads) {
+    for (int o = tid; o < 16 * D / 2; o += WAVES * kWave) {
       const int q = o / (D / 2), ch = o % (D / 2) * 2, row = row0 + 16 * n + q;
       if (row >= min(sh.R, row0 + sh.block)) continue;
       float M = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_acc[w][q][D]);
+      for (int w = 0; w < WAVES; ++w) M = fmaxf(M, sm_acc[w][q][D]);
       float a = 0.f, b = 0.f, den_q = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < WAVES; ++w) {
         const float lw = sm_acc[w][q][D + 1];
         if (lw != 0.f) {                                     // (a wavefront that saw no row has m = -inf)
           const float wgt = __builtin_amdgcn_exp2f(sm_acc[w][q][D] - M);
@@ -546,12 +545,12 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<KIND, D, NQ>())) void win
 // out[row] from its pieces, in order.  One workgroup per (unit, query row): thread (g, d) adds up every PARTS-th piece of
 // channel d, and the sums are added in order.
 template <typename Io, int D, int TILE, typename Tab>
-__global__ __launch_bounds__(kThreads) void window_reduce_kernel(const Tab tab, const WindowShape sh,
+__global__ __launch_bounds__(kReduceThreads) void window_reduce_kernel(const Tab tab, const WindowShape sh,
                                                                  const float* __restrict__ part, void* __restrict__ out) {
-  constexpr int PARTS = kThreads / D;
+  constexpr int PARTS = kReduceThreads / D;
   __shared__ float sm_w[kMaxParts];
   __shared__ float sm_num[PARTS][D];
-  __shared__ float sm_top[kWaves], sm_den[kWaves];
+  __shared__ float sm_top[(kReduceThreads / kWave)], sm_den[(kReduceThreads / kWave)];
   const CacheUnit un = tab.unit(blockIdx.x / sh.R);
   const int row = blockIdx.x % sh.R;
   const int n = parts_of(reach_of<TILE>(sh, un.len, row / sh.block).tiles, sh.part_tiles);
@@ -565,7 +564,7 @@ __global__ __launch_bounds__(kThreads) void window_reduce_kernel(const Tab tab, 
   if (tid % kWave == 0) sm_top[tid / kWave] = M;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_top[w]);
+  for (int w = 0; w < (kReduceThreads / kWave); ++w) M = fmaxf(M, sm_top[w]);
   const float wgt = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M);
   if (tid < n) sm_w[tid] = wgt;
   float den = l == 0.f ? 0.f : l * wgt;
@@ -590,7 +589,7 @@ __global__ __launch_bounds__(kThreads) void window_reduce_kernel(const Tab tab, 
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) { a += sm_num[i][2 * tid]; b += sm_num[i][2 * tid + 1]; }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) total += sm_den[w];
+    for (int w = 0; w < (kReduceThreads / kWave); ++w) total += sm_den[w];
     store_two((Io*)out + query_row(sh, un.index, row) * D + 2 * tid, quotient(a, total), quotient(b, total));
   }
 }
@@ -607,18 +606,22 @@ template <CacheKind KIND, int D, typename Tab>
 hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
                        float* part, hipStream_t stream) {
   const dim3 grid((unsigned)((long long)n_units * sh.n_blocks * sh.n_parts));
-  auto go = [&](auto nq) {
-    constexpr int NQ = decltype(nq)::value;
-    if (cache.counts) {
-      hipLaunchKernelGGL((window_rows_kernel<KIND, D, NQ, true, Tab>), grid, dim3(kThreads), 0, stream, tab, sh, cache, Q, out,
-                         part);
-    } else {
-      hipLaunchKernelGGL((window_rows_kernel<KIND, D, NQ, false, Tab>), grid, dim3(kThreads), 0, stream, tab, sh, cache, Q, out,
-                         part);
-    }
+  auto go = [&](auto nq, auto waves) {
+    constexpr int NQ = decltype(nq)::value, WAVES = decltype(waves)::value;
+    auto counted = [&](auto counts) {
+      hipLaunchKernelGGL((window_rows_kernel<KIND, D, NQ, WAVES, decltype(counts)::value, Tab>), grid, dim3(WAVES * kWave), 0,
+                         stream, tab, sh, cache, Q, out, part);
+    };
+    if (cache.counts) counted(std::true_type{});
+    else counted(std::false_type{});
   };
-  if (sh.block == 16) go(std::integral_constant<int, 1>{});
-  else go(std::integral_constant<int, 2>{});
+  auto sized = [&](auto nq) {
+    constexpr int NQ = decltype(nq)::value, MANY = 4 * waves_per_simd<KIND, D, NQ>();
+    if (sh.large) go(nq, std::integral_constant<int, MANY>{});
+    else go(nq, std::integral_constant<int, 4>{});
+  };
+  if (sh.block == 16) sized(std::integral_constant<int, 1>{});
+  else sized(std::integral_constant<int, 2>{});
   return hipGetLastError();
 }
 
@@ -656,7 +659,7 @@ hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* list
                                 bool f32, int tile, const float* part, void* out, hipStream_t stream) {
   auto go = [&](const auto& tab, auto io, auto d, auto t) {
     hipLaunchKernelGGL((window_reduce_kernel<decltype(io), decltype(d)::value, decltype(t)::value, std::decay_t<decltype(tab)>>),
-                       dim3((unsigned)((long long)n_units * sh.R)), dim3(kThreads), 0, stream, tab, sh, part, out);
+                       dim3((unsigned)((long long)n_units * sh.R)), dim3(kReduceThreads), 0, stream, tab, sh, part, out);
   };
   auto typed = [&](const auto& tab, auto d) {
     if (f32) go(tab, float{}, d, std::integral_constant<int, kWindowTile>{});
