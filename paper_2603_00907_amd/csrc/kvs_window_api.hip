@@ -134,12 +134,14 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
     for (int u = 0; u < p->n_units; ++u) bytes += 2ll * p->len[u] * sh.D * 4;
     small = small || bytes <= kStreamBytes;
   }
-  sh.block = plan->wide ? (sh.R <= 128 ? 128 : 256) : small ? 16 : 32;
+  // (of 64 channels several workgroups of 128 rows share a compute unit)
+  sh.block = plan->wide ? (sh.R <= 128 || sh.D == 64 ? 128 : 256) : small ? 16 : 32;
   sh.n_blocks = (sh.R + sh.block - 1) / sh.block;
   // Workgroups that run at once.  One per compute unit keeps memory busy with plain rows (one token on 64 caches of 8224 rows:
   // 54.7 us with 256 workgroups, 57.2 with 512, 58.2 with 768).  Of those that read rows in 4 bits as many as fit the registers
   // (64 channels, pieces of 22 and 65 tiles: 768 workgroups 18.9 us, 256 26.0; 16 query rows of 128 channels 27.4 and 37.8).
-  const int per_unit = !packed ? 1 : sh.block == 16 ? 3 : sh.block == 256 ? 1 : 2;
+  // The wide kernel's are one or two (see there).
+  const int per_unit = plan->wide ? (sh.D == 64 || (packed && sh.block == 128) ? 2 : 1) : !packed ? 1 : sh.block == 16 ? 3 : 2;
   cut_into_parts(p, plan->wide ? kWideTile : kWindowTile, kComputeUnits * per_unit, !plan->wide, sh);
   plan->equal = true;
   for (int u = 1; u < p->n_units; ++u) {

@@ -89,14 +89,17 @@ struct Staged<CacheKind::kPackedBf16, D, THREADS> {
   }
 };
 
-// Wavefronts per SIMD that the registers are allotted for.  With four wavefronts per workgroup two of those share a compute unit
-// where the pieces on their way are rows in 4 bits (8 caches of 131072 rows, 64 query rows: 86 us, one workgroup 126); those of
-// plain rows would have to be spilled (64 of 8224: 84 us, one workgroup 77).
-template <CacheKind KIND, int WAVES>
-constexpr int waves_per_simd() { return WAVES == 8 || KIND == CacheKind::kPackedBf16 ? 2 : 1; }
+// Wavefronts per SIMD that the registers are allotted for, i.e. workgroups of four wavefronts that share a compute unit.  64 channels:
+// three, with cardinalities two (a prompt of 8192 tokens 324 us with three, 352 with two, 359 with one workgroup of eight
+// wavefronts).  128 channels: two where the pieces on their way are rows in 4 bits (8 caches of 131072 rows, 64 query rows:
+// 86 us, one workgroup 126); those of plain rows would have to be spilled (64 of 8224: 84 us, one workgroup 77).
+template <CacheKind KIND, int D, int WAVES, bool COUNTS>
+constexpr int waves_per_simd() {
+  return WAVES == 8 ? 2 : D == 64 ? (COUNTS ? 2 : 3) : KIND == CacheKind::kPackedBf16 ? 2 : 1;
+}
 
 template <CacheKind KIND, int D, int WAVES, bool COUNTS, typename Tab>
-__global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, WAVES>())) void window_tiles_kernel(
+__global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, WAVES, COUNTS>())) void window_tiles_kernel(
     const Tab tab, const WindowShape sh, const Cache cache, int n_units, const uint16_t* __restrict__ Q,
     uint16_t* __restrict__ out, float* __restrict__ part) {
   constexpr int kThreads = WAVES * kWave;
@@ -385,10 +388,7 @@ hipError_t launch_waves(const Tab& tab, int n_units, const WindowShape& sh, cons
 template <CacheKind KIND, typename Tab>
 hipError_t launch_sized(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
                         float* part, hipStream_t stream) {
-  if (sh.D == 64) {
-    return sh.block == 128 ? launch_waves<KIND, 64, 4>(tab, n_units, sh, cache, Q, out, part, stream)
-                           : launch_waves<KIND, 64, 8>(tab, n_units, sh, cache, Q, out, part, stream);
-  }
+  if (sh.D == 64) return launch_waves<KIND, 64, 4>(tab, n_units, sh, cache, Q, out, part, stream);
   return sh.block == 128 ? launch_waves<KIND, 128, 4>(tab, n_units, sh, cache, Q, out, part, stream)
                          : launch_waves<KIND, 128, 8>(tab, n_units, sh, cache, Q, out, part, stream);
 }
