@@ -27,7 +27,6 @@ struct ListedUnits {
   CacheUnit u[kInlineUnits];
   __device__ __forceinline__ CacheUnit unit(int i) const {
 #if defined(__HIP_DEVICE_COMPILE__)
-    // (the index is uniform over the workgroup: scalar loads)
     if (ext != nullptr) return ((const __attribute__((address_space(4))) CacheUnit*)ext)[i];
 #endif
     return u[i];

@@ -66,43 +66,93 @@ long long tiles_bound(const WindowShape& sh, int len, int tile) {
   return tiles(std::min<long long>(len, sh.span + positions - 1)) + tiles(std::min(sh.sinks, len));
 }
 
-// How the rows that a block sees are cut into pieces: the longest that make no more workgroups than run at once, `at_once`
-// (all of a call's workgroups take as long, and what one does for its piece, a partial result written and read again, is done
-// as rarely as possible).
-void cut_into_parts(const kvs_problem* p, int tile, long long at_once, bool can_be_large, WindowShape& sh) {
-  constexpr long long kLeastTiles = 4;           // a tile for each wavefront of a workgroup, or as much work as that
-  long long most = 1;
-  for (int u = 0; u < p->n_units; ++u) most = std::max(most, tiles_bound(sh, p->len[u], tile));
+// How the rows that a block of query rows sees are cut into pieces, of at most kMaxParts.
+struct Cut {
+  const kvs_problem* p;
+  const WindowShape& sh;
+  int tile;
+  long long most = 1;                            // tiles of the longest reach
+  bool equal = true;                             // reaches of one length
+  Cut(const kvs_problem* problem, const WindowShape& shape, int rows) : p(problem), sh(shape), tile(rows) {
+    for (int u = 0; u < p->n_units; ++u) {
+      most = std::max(most, tiles_bound(sh, p->len[u], tile));
+      equal = equal && p->len[u] == p->len[0];
+    }
+  }
+  // workgroups of a call whose pieces have `per` tiles at most; *tiles: those of all of them
+  long long workgroups(long long per, long long* tiles = nullptr) const {
+    long long n = 0, sum = 0, parts = 0, t = 0;
+    const int units = equal ? 1 : p->n_units;
+    for (int u = 0; u < units; ++u) {
+      if (u == 0 || p->len[u] != p->len[u - 1]) {
+        t = tiles_bound(sh, p->len[u], tile);
+        parts = std::max(1ll, (t + per - 1) / per);
+      }
+      n += parts * sh.n_blocks;
+      sum += t * sh.n_blocks;
+    }
+    const long long times = equal ? p->n_units : 1;
+    if (tiles) *tiles = sum * times;
+    return n * times;
+  }
+};
+
+// kvs_window_rows.hip: the longest pieces that make no more workgroups than run at once, since memory bounds all of them alike and
+// what one does for its piece, a partial result written and read again, is done as rarely as possible.
+void cut_rows(const kvs_problem* p, long long at_once, WindowShape& sh) {
+  const Cut cut(p, sh, kWindowTile);
   // A workgroup of all the wavefronts that a compute unit holds for a whole reach, which spares the partial results: where there
   // is one for most compute units (one token on 256 caches of 4096 slots in 4 bits 35.8 us, in three pieces each 41.2), and for
   // reaches that are a round or two of its tiles (8 caches of 300 rows 8.0 us, in pieces 9.2; of 777 rows 12.0 and 9.4).
   const long long whole = (long long)p->n_units * sh.n_blocks;
-  if (can_be_large && whole <= kComputeUnits && (most <= 12 || whole >= kComputeUnits * 3 / 4)) {
+  if (whole <= kComputeUnits && (cut.most <= 12 || whole >= kComputeUnits * 3 / 4)) {
     sh.large = 1;
-    sh.part_tiles = (int)most;
+    sh.part_tiles = (int)cut.most;
     sh.n_parts = 1;
     return;
   }
-  auto workgroups = [&](long long per) {
-    long long n = 0, parts = 0;
-    for (int u = 0; u < p->n_units; ++u) {
-      if (u == 0 || p->len[u] != p->len[u - 1]) parts = std::max(1ll, (tiles_bound(sh, p->len[u], tile) + per - 1) / per);
-      n += parts * sh.n_blocks;
-    }
-    return n;
-  };
-  long long per = std::max(kLeastTiles, (most + kMaxParts - 1) / kMaxParts);
-  if (workgroups(per) > at_once) {
-    long long fits = std::max(per, most);        // (whole reaches, whether or not they fit)
+  constexpr long long kLeastTiles = 4;           // a tile for each wavefront of a workgroup
+  long long per = std::max(kLeastTiles, (cut.most + kMaxParts - 1) / kMaxParts);
+  if (cut.workgroups(per) > at_once) {
+    long long fits = std::max(per, cut.most);    // (whole reaches, whether or not they fit)
     while (fits - per > 1) {
       const long long mid = (per + fits) / 2;
-      if (workgroups(mid) > at_once) per = mid;
+      if (cut.workgroups(mid) > at_once) per = mid;
       else fits = mid;
     }
     per = fits;
   }
   sh.part_tiles = (int)per;
-  sh.n_parts = (int)((most + per - 1) / per);
+  sh.n_parts = (int)((cut.most + per - 1) / per);
+}
+
+// kvs_window_tiles.hip, whose workgroups keep a compute unit busy by themselves and whose partial results are many: the number of
+// pieces with the shortest time, counted in tiles.  A workgroup takes kOnce tiles' time besides its tiles, and pieces cost a
+// launch that adds them up and their partials' way to memory and back.  (512 tokens of 32 heads on 8, 16 and 24 caches of 9000
+// rows: 95 us in four pieces, 173 in two (whole 265) and 268 whole; 24 of 2250 to 9000 245, whole 258, in the longest pieces of
+// at most 256 workgroups 378.)
+void cut_tiles(const kvs_problem* p, long long at_once, WindowShape& sh) {
+  constexpr long long kOnce = 3;
+  constexpr double kTileUs = 2.06, kLaunchUs = 6, kBytesPerUs = 4e6;
+  const Cut cut(p, sh, kWideTile);
+  double best = 0;
+  for (long long n = 1; n <= 32; ++n) {
+    const long long per = std::max(4ll, (cut.most + n - 1) / n);
+    long long tiles = 0;
+    const long long groups = cut.workgroups(per, &tiles);
+    double time = cut.equal ? (double)((groups + at_once - 1) / at_once * (per + kOnce))
+                            : (double)(tiles + groups * kOnce) / at_once + (double)(per + kOnce) / 2;
+    if (n > 1) {
+      const double partials = 8.0 * p->n_units * sh.R * (sh.D + 2) * (double)((cut.most + per - 1) / per);
+      time += (kLaunchUs + partials / kBytesPerUs) / kTileUs;
+    }
+    if (n == 1 || time < best) {
+      best = time;
+      sh.part_tiles = (int)per;
+      sh.n_parts = (int)((cut.most + per - 1) / per);
+    }
+    if (per == 4 || (n == 1 && groups >= 8 * at_once)) break;   // (nothing to gain)
+  }
 }
 
 kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, WindowPlan* plan, int* elt) {
@@ -142,7 +192,8 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
   // (64 channels, pieces of 22 and 65 tiles: 768 workgroups 18.9 us, 256 26.0; 16 query rows of 128 channels 27.4 and 37.8).
   // The wide kernel's are one or two (see there).
   const int per_unit = plan->wide ? (sh.D == 64 || (packed && sh.block == 128) ? 2 : 1) : !packed ? 1 : sh.block == 16 ? 3 : 2;
-  cut_into_parts(p, plan->wide ? kWideTile : kWindowTile, kComputeUnits * per_unit, !plan->wide, sh);
+  if (plan->wide) cut_tiles(p, kComputeUnits * per_unit, sh);
+  else cut_rows(p, kComputeUnits * per_unit, sh);
   plan->equal = true;
   for (int u = 1; u < p->n_units; ++u) {
     plan->equal = plan->equal && p->len[u] == p->len[0] && p->in_row[u] - p->in_row[u - 1] == p->in_row[1] - p->in_row[0];
@@ -154,16 +205,13 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
   return KVS_OK;
 }
 
-// One size for both forms.
-kvs_status window_workspace(const kvs_problem* p, int32_t span, size_t* bytes) {
-  *bytes = 0;
-  for (const bool packed : {false, true}) {
-    WindowPlan plan;
-    int elt = 0;
-    const kvs_status st = make_window_plan(p, span, packed, &plan, &elt);
+// The plans of both forms, [0] of the plain one, and the size of the workspace that serves both.
+kvs_status make_window_plans(const kvs_problem* p, int32_t span, WindowPlan (&plans)[2], int* elt, size_t* bytes) {
+  for (const int packed : {0, 1}) {
+    const kvs_status st = make_window_plan(p, span, packed != 0, &plans[packed], elt);
     if (st != KVS_OK) return st;
-    *bytes = std::max(*bytes, plan.bytes());
   }
+  *bytes = std::max(plans[0].bytes(), plans[1].bytes());
   return KVS_OK;
 }
 
@@ -177,13 +225,13 @@ struct Buffers {
 
 kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, const void* Q, const Cache& cache, void* out,
                             void* ws, size_t ws_bytes, void* hip_stream) {
-  WindowPlan plan;
+  WindowPlan plans[2];
   int elt = 0;
-  kvs_status st = make_window_plan(p, span, packed, &plan, &elt);
-  if (st != KVS_OK) return st;
-  const WindowShape& sh = plan.sh;
   size_t need = 0;
-  if ((st = window_workspace(p, span, &need)) != KVS_OK) return st;
+  kvs_status st = make_window_plans(p, span, plans, &elt, &need);
+  if (st != KVS_OK) return st;
+  const WindowPlan& plan = plans[packed];
+  const WindowShape& sh = plan.sh;
   if (need > 0 && (ws == nullptr || ((uintptr_t)ws % kAlign) != 0 || ws_bytes < need)) return KVS_ERR_WORKSPACE;
   const size_t rows = rows_to(p, p->in_row), qo = (size_t)p->n_units * sh.R * sh.D * elt;
   const size_t row_bytes = packed ? (size_t)sh.D / 2 : (size_t)sh.D * elt;
@@ -316,8 +364,10 @@ extern "C" {
 
 kvs_status kvs_window_attention_workspace_size(const kvs_problem* p, int32_t span, size_t* bytes) {
   if (bytes == nullptr) return KVS_ERR_INVALID_ARG;
+  WindowPlan plans[2];
+  int elt = 0;
   size_t need = 0;
-  const kvs_status st = window_workspace(p, span, &need);
+  const kvs_status st = make_window_plans(p, span, plans, &elt, &need);
   if (st == KVS_OK) *bytes = need;
   return st;
 }

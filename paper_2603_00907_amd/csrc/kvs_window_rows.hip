@@ -594,6 +594,43 @@ __global__ __launch_bounds__(kReduceThreads) void window_reduce_kernel(const Tab
   }
 }
 
+// The same where no reach has more than kFewParts pieces: a thread takes two channels of a query row and requests everything at
+// once, so that the partials cost one round trip and nobody meets.
+constexpr int kFewParts = 8;
+template <typename Io, int D, int TILE, typename Tab>
+__global__ __launch_bounds__(kReduceThreads) void window_reduce_few_kernel(const Tab tab, const WindowShape sh, int n_rows,
+                                                                           const float* __restrict__ part,
+                                                                           void* __restrict__ out) {
+  constexpr int PER = D / 2;               // threads per row
+  const int at = (int)blockIdx.x * (kReduceThreads / PER) + (int)threadIdx.x / PER, ch = (int)threadIdx.x % PER * 2;
+  if (at >= n_rows) return;
+  const CacheUnit un = tab.unit(at / sh.R);
+  const int row = at % sh.R;
+  const int n = parts_of(reach_of<TILE>(sh, un.len, row / sh.block).tiles, sh.part_tiles);
+  const float* src = part + part_at(sh, un.index, row, 0);
+  float2 x[kFewParts], ml[kFewParts];
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) {
+    const float* p = src + min(i, n - 1) * (D + 2);
+    x[i] = *(const float2*)(p + ch);
+    ml[i] = *(const float2*)(p + D);
+  }
+  float M = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) M = fmaxf(M, ml[i].x);
+  float a = 0.f, b = 0.f, den = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) {
+    if (i < n && ml[i].y != 0.f) {
+      const float wgt = __builtin_amdgcn_exp2f(ml[i].x - M);
+      a = fmaf(x[i].x, wgt, a);
+      b = fmaf(x[i].y, wgt, b);
+      den = fmaf(ml[i].y, wgt, den);
+    }
+  }
+  store_two((Io*)out + query_row(sh, un.index, row) * D + ch, quotient(a, den), quotient(b, den));
+}
+
 // Unit descriptors of a launch that has too many for its arguments, stored by a kernel that carries some in its own.
 constexpr int kTableBatch = 224;
 struct CacheUnitBatch { CacheUnit u[kTableBatch]; };
@@ -657,9 +694,17 @@ hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed
 
 hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
                                 bool f32, int tile, const float* part, void* out, hipStream_t stream) {
+  const int rows = n_units * sh.R;
   auto go = [&](const auto& tab, auto io, auto d, auto t) {
-    hipLaunchKernelGGL((window_reduce_kernel<decltype(io), decltype(d)::value, decltype(t)::value, std::decay_t<decltype(tab)>>),
-                       dim3((unsigned)((long long)n_units * sh.R)), dim3(kReduceThreads), 0, stream, tab, sh, part, out);
+    constexpr int D = decltype(d)::value, TILE = decltype(t)::value, PER = kReduceThreads / (D / 2);
+    typedef std::decay_t<decltype(tab)> Tab;
+    if (sh.n_parts <= kFewParts) {
+      hipLaunchKernelGGL((window_reduce_few_kernel<decltype(io), D, TILE, Tab>), dim3((rows + PER - 1) / PER),
+                         dim3(kReduceThreads), 0, stream, tab, sh, rows, part, out);
+    } else {
+      hipLaunchKernelGGL((window_reduce_kernel<decltype(io), D, TILE, Tab>), dim3(rows), dim3(kReduceThreads), 0, stream, tab,
+                         sh, part, out);
+    }
   };
   auto typed = [&](const auto& tab, auto d) {
     if (f32) go(tab, float{}, d, std::integral_constant<int, kWindowTile>{});
