@@ -31,7 +31,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = kWideTile;
 // A lane's sixteen terms may add up to this before their reference is raised to the largest logit.
-constexpr float kMostSum = 65536.f;
+constexpr float kMostSum = 1024.f;
 
 // Where piece `p` (16 bytes) of row r is within its row.
 template <int D> __device__ __forceinline__ int key_slot(int r, int p) { return D == 128 ? p ^ (r % 16) : p ^ (r / 2 % 8); }

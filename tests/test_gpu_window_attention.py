@@ -129,12 +129,47 @@ def test_many_units_equal_and_not(dtype, packed):
     check(lens=[600 + 5 * i for i in range(70)], G=4, W=1, D=64, dtype=dtype, packed=packed, counts=True)
 
 
+@pytest.mark.parametrize("dtype,packed", CACHES)
+@pytest.mark.parametrize("lens,G,W,counts", [([9000], 4, 40, True), ([5000, 700], 4, 70, False), ([12000] * 2, 5, 9, True)])
+def test_many_query_rows_on_long_caches(dtype, packed, lens, G, W, counts):
+    """Pieces of the wide kernel's reaches, in blocks of 128 and 256 rows."""
+    check(lens=lens, G=G, W=W, D=128, dtype=dtype, packed=packed, counts=counts, sinks=3)
+    check(lens=lens, G=G, W=W, D=64, dtype=dtype, packed=packed, counts=not counts, span=4000, sinks=3)
+
+
+@pytest.mark.parametrize("dtype,packed", CACHES)
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_workgroup_per_cache(dtype, packed, D):
+    """One for most compute units, reaches of more tiles than it has wavefronts."""
+    check(lens=[500] * 200, G=4, W=1, D=D, dtype=dtype, packed=packed, counts=True)
+    check(lens=[500 + i % 3 for i in range(192)], G=6, W=4, D=D, dtype=dtype, packed=packed, span=450, sinks=2)
+
+
+@pytest.mark.parametrize("dtype,packed", CACHES)
+@pytest.mark.parametrize("G,W", [(4, 1), (4, 8), (3, 20), (4, 60)])
+@pytest.mark.parametrize("rising", [True, False])
+def test_logits_that_rise_or_fall_along_the_cache(dtype, packed, G, W, rising):
+    """Every later row outweighs all before it by hundreds of powers of two in the end, or the first rows all behind them."""
+    call = Call(13, lens=[700, 64], G=G, W=W, D=128, dtype=dtype, packed=packed, scale=1.0)
+    call.Q = np.abs(call.Q)
+    for n, r in zip(call.lens, call.first):
+        ramp = np.linspace(0, 8, n) if rising else np.linspace(8, 0, n)
+        K = 0.1 * call.K[r:r + n] + ramp[:, None]
+        call.K[r:r + n] = R.bf16(K) if dtype == "bf16" else K
+    if packed:
+        call.codes[:2] = R.pack(call.K.astype(np.float32))
+        call.K = R.unpack(*call.codes[:2])
+    call.launch().run()
+    call.check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("G,W,n", [(4, 300, 300), (1, 513, 700), (4, 256, 1024), (7, 100, 260), (2, 130, 65)])
 @pytest.mark.parametrize("span,sinks", [(0, 0), (100, 4), (20, 0), (64, 65)])
 def test_prompts_and_chunks(dtype, G, W, n, span, sinks):
     check(lens=[n, n // 2], G=G, W=W, D=128, dtype=dtype, span=span, sinks=sinks)
     check(lens=[n], G=G, W=W, D=64, dtype=dtype, span=span, sinks=sinks, counts=True)
+    check(lens=[n, 3], G=G, W=W, D=64, dtype=dtype, span=span, sinks=sinks, packed=span == 20)
 
 
 @pytest.mark.parametrize("dtype,packed", CACHES)

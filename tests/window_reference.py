@@ -53,7 +53,9 @@ def attention(Q, K, V, *, causal, span, sinks, counts=None, scale=0.0, weight_bi
     The bound: a logit is a sum of D products (fp32 partial sums: D roundings of 2^-24 of the sum of magnitudes, and two
     more for the scale), the exponential and its argument round four times, the weight is taken with `weight_bits` bits, and
     both sums add up at most n terms in any order.  Every weight's relative error counts once in the numerator and once in
-    the denominator.  The output is rounded to `out_bits` bits."""
+    the denominator.  The output is rounded to `out_bits` bits.  Below 2^-126 the types have no numbers of full precision: a
+    term of which the largest is more than 2^126 times (or 2^118, where the reference is up to 2^8 above it) may be lost
+    whole, and so may a result of that size."""
     Q, K, V = (np.asarray(x, dtype=np.float64) for x in (Q, K, V))
     G, W, D = Q.shape
     n = K.shape[0]
@@ -75,6 +77,7 @@ def attention(Q, K, V, *, causal, span, sinks, counts=None, scale=0.0, weight_bi
             rel = (D + 2) * u * size + 4 * u * (1 + np.abs(e - e.max(1, keepdims=True))) + 2.0 ** -weight_bits + len(at) * u
             off[:, w] = (p * rel) @ np.abs(V[at]) / den + (p * rel * c[at]).sum(1, keepdims=True) / den * np.abs(out[:, w])
             off[:, w] += 2.0 ** -out_bits * np.abs(out[:, w])
+            off[:, w] += 2.0 ** -126 + len(at) * 2.0 ** -118 * np.abs(V[at]).max(0)
     return out, off
 
 
