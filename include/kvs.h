@@ -278,7 +278,8 @@ kvs_status kvs_step_per_query_counts(const kvs_problem* p, const void* Q, const 
  *   K, V    DEVICE in  [rows, D] io_dtype
  *   counts  DEVICE in  [rows] i32, every entry >= 1, or NULL for a cache of plain tokens
  *   out     DEVICE out [n_units, G, W, D] io_dtype: sums in fp32, rounded once; with KVS_BF16 the weights exp(e_t) enter the
- *           product with V as bf16 numbers or sums of two of them, with KVS_F32 as sums of three or as they are
+ *           product with V as bf16 numbers or sums of two of them, with KVS_F32 as sums of three or as they are; cardinalities
+ *           above 65536 may be taken to 2^-16
  *   ws      DEVICE workspace of kvs_window_attention_workspace_size(p, span) bytes, 256-byte aligned; NULL is fine where that
  *           is 0 (KVS_ERR_WORKSPACE).  It serves both forms.
  * Asynchronous on hip_stream; nothing is allocated; errors are found on the host before any launch.                       */

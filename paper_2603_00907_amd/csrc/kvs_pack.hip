@@ -2,7 +2,10 @@
 //
 // Both are copies: memory bounds them, 2 D bytes (bf16) against D / 2 + D / 32 for each of K and V.  A thread takes eight
 // neighbouring values of a row of K and the same of V, so that the lanes of a wavefront cover whole rows; the four threads
-// of a block of 32 exchange the largest magnitude by lane moves.
+// of a block of 32 exchange the largest magnitude by lane moves.  One row per thread: the wavefronts of many short workgroups
+// have as much on its way as memory takes, and several rows per thread are slower (256 caches of 4096 bf16 rows of 128 channels,
+// 679 MB: packing 116 us, 5.8 TB/s, 120 with two rows and 124 with four; unpacking 120; 100 fp32 caches of unequal lengths up to
+// 9000 rows of 64 channels 66 and 64 us, with four rows 68 and 96).
 #include "kvs_fp4.h"
 #include "kvs_pack.h"
 
@@ -11,9 +14,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kEach = 8;                 // values per thread and row
-constexpr int kSteps = 4;                // rows per thread, all loads issued before the first use
-template <int D> constexpr int rows_per_step() { return kThreads * kEach / D; }
-template <int D> constexpr int rows_per_group() { return rows_per_step<D>() * kSteps; }
+template <int D> constexpr int rows_per_group() { return kThreads * kEach / D; }
 
 template <typename T> struct Eight;
 template <> struct Eight<uint16_t> {
@@ -62,33 +63,23 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const Tab tab, const T* 
                                                         uint8_t* __restrict__ kc, uint8_t* __restrict__ ks,
                                                         uint8_t* __restrict__ vc, uint8_t* __restrict__ vs) {
   const RowMove mv = tab.unit(blockIdx.y);
-  const int r = (int)blockIdx.x * rows_per_group<D>() + (int)threadIdx.x * kEach / D;
+  const int row = (int)blockIdx.x * rows_per_group<D>() + (int)threadIdx.x * kEach / D;
   const int ch = (int)threadIdx.x * kEach % D;
-  if ((int)blockIdx.x * rows_per_group<D>() >= mv.len) return;
-  Eight<T> k[kSteps], v[kSteps];
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const size_t at = ((size_t)mv.src + min(r + i * rows_per_step<D>(), mv.len - 1)) * D + ch;
-    k[i].load(K + at);
-    v[i].load(V + at);
-  }
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int row = r + i * rows_per_step<D>();
-    float x[8], y[8];
-    k[i].unpack(x);
-    v[i].unpack(y);
-    uint32_t sx, sy;
-    const uint32_t cx = encode(x, sx), cy = encode(y, sy);
-    if (row < mv.len) {
-      const size_t at = ((size_t)mv.dst + row) * D + ch;
-      *(uint32_t*)(kc + at / 2) = cx;
-      *(uint32_t*)(vc + at / 2) = cy;
-      if (ch % fp4::kBlock == 0) {
-        ks[at / fp4::kBlock] = (uint8_t)sx;
-        vs[at / fp4::kBlock] = (uint8_t)sy;
-      }
-    }
+  if (row >= mv.len) return;               // (a row's threads go together)
+  const size_t from = ((size_t)mv.src + row) * D + ch, to = ((size_t)mv.dst + row) * D + ch;
+  Eight<T> k, v;
+  k.load(K + from);
+  v.load(V + from);
+  float x[8], y[8];
+  k.unpack(x);
+  v.unpack(y);
+  uint32_t sx, sy;
+  const uint32_t cx = encode(x, sx), cy = encode(y, sy);
+  *(uint32_t*)(kc + to / 2) = cx;
+  *(uint32_t*)(vc + to / 2) = cy;
+  if (ch % fp4::kBlock == 0) {
+    ks[to / fp4::kBlock] = (uint8_t)sx;
+    vs[to / fp4::kBlock] = (uint8_t)sy;
   }
 }
 
@@ -98,31 +89,18 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const Tab tab, const u
                                                           const uint8_t* __restrict__ vs, T* __restrict__ K,
                                                           T* __restrict__ V) {
   const RowMove mv = tab.unit(blockIdx.y);
-  const int r = (int)blockIdx.x * rows_per_group<D>() + (int)threadIdx.x * kEach / D;
+  const int row = (int)blockIdx.x * rows_per_group<D>() + (int)threadIdx.x * kEach / D;
   const int ch = (int)threadIdx.x * kEach % D;
-  if ((int)blockIdx.x * rows_per_group<D>() >= mv.len) return;
-  uint32_t c[2][kSteps];
-  uint8_t s[2][kSteps];
+  if (row >= mv.len) return;
+  const size_t from = ((size_t)mv.src + row) * D + ch, to = ((size_t)mv.dst + row) * D + ch;
+  const uint32_t c[2] = {*(const uint32_t*)(kc + from / 2), *(const uint32_t*)(vc + from / 2)};
+  const uint8_t s[2] = {ks[from / fp4::kBlock], vs[from / fp4::kBlock]};
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const size_t at = ((size_t)mv.src + min(r + i * rows_per_step<D>(), mv.len - 1)) * D + ch;
-    c[0][i] = *(const uint32_t*)(kc + at / 2);
-    c[1][i] = *(const uint32_t*)(vc + at / 2);
-    s[0][i] = ks[at / fp4::kBlock];
-    s[1][i] = vs[at / fp4::kBlock];
-  }
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int row = r + i * rows_per_step<D>();
-    if (row >= mv.len) break;
-    const size_t at = ((size_t)mv.dst + row) * D + ch;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float scale = fp4::scale_of(s[x][i]);
-      const uint32_t w[4] = {fp4::two_of<0>(c[x][i], scale), fp4::two_of<1>(c[x][i], scale),
-                             fp4::two_of<2>(c[x][i], scale), fp4::two_of<3>(c[x][i], scale)};
-      Eight<T>::store((x == 0 ? K : V) + at, w);
-    }
+  for (int x = 0; x < 2; ++x) {
+    const float scale = fp4::scale_of(s[x]);
+    const uint32_t w[4] = {fp4::two_of<0>(c[x], scale), fp4::two_of<1>(c[x], scale), fp4::two_of<2>(c[x], scale),
+                           fp4::two_of<3>(c[x], scale)};
+    Eight<T>::store((x == 0 ? K : V) + to, w);
   }
 }
 

@@ -1,19 +1,25 @@
-// The attention of kvs_window_rows.hip for blocks of many query rows, bf16 ones: a prompt, or a chunk of new tokens on a cache.
-// Rows in 4 bits become bf16 on their way into LDS.
+// The attention of kvs_window_rows.hip for more than 32 bf16 query rows: a prompt, a chunk of new tokens on a cache, drafts of many
+// heads.  Rows in 4 bits become bf16 on their way into LDS.
 //
 // What bounds it is the matrix cores (4 D operations per query and row against 4 D bytes per row of the cache), so tiles of 64
-// cache rows go through LDS, once for the 128 NB query rows of a workgroup, and every operand read feeds NB products.
-// A wavefront takes 32 NB query rows:
+// cache rows go through LDS, once for the 128 or 256 query rows of a workgroup.  A wavefront takes 32 query rows, and a tile in
+// two halves of 32 cache rows:
 //   S[t, q] = K Q^T on v_mfma_f32_32x32x16_bf16: a lane holds one query column and 16 of 32 rows, so that the softmax of a
 //             column is the lane's and its partner's (half a wavefront away) alone;
-//   O^T[d, q] += V^T P: P is in operand order as it leaves the softmax, rounded to one bf16 number (its error, at most 2^-9 of
+//   O^T[d, q] += V^T P: P is in operand order as it leaves the softmax, rounded to one bf16 number (its error, at most 2^-8 of
 //             each weight and of any sign, disappears in the sum beside the rounding of the output), and V^T comes from LDS by
 //             transposing reads.
-// The next 32 rows' products with Q are issued beside the exponentials of the 32 rows at hand.  One barrier per tile: while
-// tile j is worked on, K of tile j + 2 and V of tile j + 1 travel from memory into those of the six buffers in LDS that
-// nobody reads.  (Six arrays, and every access to one that is known at compile time: the compiler then waits for a load into LDS where its
-// array is read, and not at every read.)
-// Pieces of 16 bytes are swizzled within a row of LDS so that neither kind of read meets a bank twice.
+// A half's exponentials are issued beside the next half's products with Q, whose K operands were read a half before: the
+// transcendental unit (16 cycles per instruction), the other vector work and the matrix cores are each busy for about 256, 260
+// and 512 cycles of a half.  There is no maximum per half: terms are formed against the reference at hand, and only a sum that
+// is too large (or not a number) has the largest logit looked for.  One barrier per tile: while tile j is worked on, K of tile
+// j + 2 and V of tile j + 1 travel through registers into the buffers of LDS that nobody reads.  Pieces of 16 bytes are
+// swizzled within a row of LDS so that neither kind of read meets a bank twice (no conflicts counted).
+// Measured on a prompt of 8192 tokens, 32 heads of 128 channels, causal (0.55 TFLOP): 530 to 560 us on different cards, 0.98 to
+// 1.04 PFLOP/s where a large matrix product reaches 1.29; matrix cores busy for 0.48 of the cycles.  Without memory, LDS and
+// barrier it would take 409.  Slower: the products and their exponentials one after the other with all operands read ahead
+// (576), loads straight into LDS (545; the transposing reads then wait for all of them, or have to be assembly), 64 query rows
+// per wavefront at one wavefront per SIMD (1016), and a maximum per half with two products in a chain of their own (571).
 #include <type_traits>
 
 #include "kvs_window.h"
@@ -23,10 +29,8 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = kWideTile;
@@ -108,7 +112,7 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, WAVES, COUN
   constexpr int PPR = D / 8;                // pieces per row
   constexpr int PER = kTile * PPR / kThreads;    // pieces per thread of a tile of K, and of V
   __shared__ u32x4 sm_k[2][kTile * PPR], sm_v[2][kTile * PPR];
-  // cardinalities as pairs hi + lo of bf16 numbers (exact up to 65536, to 2^-17 beyond): of four rows both hi pairs, then both lo
+  // cardinalities as pairs hi + lo of bf16 numbers (exact up to 65536, to 2^-16 beyond): of four rows both hi pairs, then both lo
   __shared__ u32x4 sm_cnt[2][kTile / 4];
 
   // A unit's workgroups are n_units apart, which puts them on one XCD where n_units is a multiple of eight, and the last
