@@ -137,7 +137,7 @@ hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* liste
 // out from the partial results of kernels whose tiles have `tile` rows (kWindowTile or kWideTile).
 hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
                                 bool f32, int tile, const float* part, void* out, hipStream_t stream);
-// Descriptors of the units from `first` on into the workspace.
-hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, CacheUnit* dst, hipStream_t stream);
+// Descriptors of all units into the workspace.
+hipError_t launch_window_table(const kvs_problem* p, CacheUnit* dst, hipStream_t stream);
 
 }  // namespace kvs

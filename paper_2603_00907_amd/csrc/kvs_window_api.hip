@@ -112,12 +112,14 @@ void cut_rows(const kvs_problem* p, long long at_once, WindowShape& sh) {
     return;
   }
   constexpr long long kLeastTiles = 4;           // a tile for each wavefront of a workgroup
+  // (more units than that: whole reaches, or the longest of unequal ones cut)
+  const long long limit = whole <= at_once ? at_once : cut.equal ? whole : whole + at_once;
   long long per = std::max(kLeastTiles, (cut.most + kMaxParts - 1) / kMaxParts);
-  if (cut.workgroups(per) > at_once) {
-    long long fits = std::max(per, cut.most);    // (whole reaches, whether or not they fit)
+  if (cut.workgroups(per) > limit) {
+    long long fits = std::max(per, cut.most);
     while (fits - per > 1) {
       const long long mid = (per + fits) / 2;
-      if (cut.workgroups(mid) > at_once) per = mid;
+      if (cut.workgroups(mid) > limit) per = mid;
       else fits = mid;
     }
     per = fits;
@@ -136,7 +138,8 @@ void cut_tiles(const kvs_problem* p, long long at_once, WindowShape& sh) {
   constexpr double kTileUs = 2.06, kLaunchUs = 6, kBytesPerUs = 4e6;
   const Cut cut(p, sh, kWideTile);
   double best = 0;
-  for (long long n = 1; n <= 32; ++n) {
+  // (1, 2, 3, 4, 6, 8, 12, 16, .. pieces)
+  for (long long n = 1; n <= kMaxParts; n = n < 3 ? n + 1 : (n & (n - 1)) != 0 ? n / 3 * 4 : n / 2 * 3) {
     const long long per = std::max(4ll, (cut.most + n - 1) / n);
     long long tiles = 0;
     const long long groups = cut.workgroups(per, &tiles);
@@ -256,7 +259,7 @@ kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, con
   if (plan.table_bytes > 0) {
     CacheUnit* dst = (CacheUnit*)((char*)ws + plan.part_bytes);
     table = dst;
-    e = launch_window_table(p, 0, p->n_units, dst, s);
+    e = launch_window_table(p, dst, s);
   }
   const CacheKind kind = elt == 4 ? (packed ? CacheKind::kPackedF32 : CacheKind::kF32)
                                   : (packed ? CacheKind::kPackedBf16 : CacheKind::kBf16);

@@ -724,11 +724,11 @@ hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* list
   return hipGetLastError();
 }
 
-hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, CacheUnit* dst, hipStream_t stream) {
-  for (int at = 0; at < n_units; at += kTableBatch) {
-    const int n = n_units - at < kTableBatch ? n_units - at : kTableBatch;
+hipError_t launch_window_table(const kvs_problem* p, CacheUnit* dst, hipStream_t stream) {
+  for (int at = 0; at < p->n_units; at += kTableBatch) {
+    const int n = p->n_units - at < kTableBatch ? p->n_units - at : kTableBatch;
     CacheUnitBatch batch;
-    for (int i = 0; i < kTableBatch; ++i) batch.u[i] = cache_unit(p, first + at + (i < n ? i : 0));
+    for (int i = 0; i < kTableBatch; ++i) batch.u[i] = cache_unit(p, at + (i < n ? i : 0));
     hipLaunchKernelGGL(cache_unit_table_kernel, dim3(1), dim3(256), 0, stream, batch, n, dst + at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -30,10 +30,10 @@ namespace kvs {
 
 int debug_switch(kvs_debug_switch) { return 0; }
 
-hipError_t launch_window_table(const kvs_problem* p, int first, int n_units, CacheUnit* dst, hipStream_t) {
-  CHECK((char*)dst >= g_ws && (char*)(dst + n_units) <= g_ws + g_ws_bytes);
+hipError_t launch_window_table(const kvs_problem* p, CacheUnit* dst, hipStream_t) {
+  CHECK((char*)dst >= g_ws && (char*)(dst + p->n_units) <= g_ws + g_ws_bytes);
   g_table.clear();
-  for (int i = 0; i < n_units; ++i) g_table.push_back(cache_unit(p, first + i));
+  for (int i = 0; i < p->n_units; ++i) g_table.push_back(cache_unit(p, i));
   return hipSuccess;
 }
 

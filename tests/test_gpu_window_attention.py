@@ -245,6 +245,25 @@ def test_a_key_that_is_not_a_number_reaches_the_queries_that_see_it(dtype, packe
     assert (np.abs(got[0] - want) <= off)[:, ~touched].all()
 
 
+@pytest.mark.parametrize("dtype,packed", [("bf16", False), ("f32", True)])
+@pytest.mark.parametrize("G,W", [(4, 1), (4, 40)])
+def test_rows_more_than_four_gigabytes_into_the_cache(dtype, packed, G, W):
+    import torch
+    import paper_2603_00907_amd as kvs
+    D, at, n = 128, (1 << 24) + 12345, 700          # (2^24 rows of 256 bytes; in 4 bits twice as many of 64 and 4)
+    at = 8 * at if packed else at
+    call = Call(14, lens=[n], G=G, W=W, D=D, dtype=dtype, packed=packed).launch()
+    far = []
+    for x in call.cache:
+        y = torch.empty((at + n, x.shape[1]), dtype=x.dtype, device="cuda")
+        y[at:] = x[:n]
+        far.append(y)
+    call.cache = far
+    call.problem = kvs.Problem(lens=[n], budgets=[n], group=G, window=W, head_dim=D, dtype=dtype, in_rows=[at], causal=True)
+    call.run()
+    call.check()
+
+
 @pytest.mark.parametrize("dtype,packed", CACHES)
 def test_units_may_share_rows(dtype, packed):
     """A prefix in common: the second unit's rows are the first one's and its own behind them."""
