@@ -5,34 +5,6 @@
 
 namespace kvs {
 
-// One unit of a launch: its rows of the cache.
-struct CacheUnit {
-  long long in_row;
-  int len;
-  int index;            // position in the caller's problem (indexes Q, out, partials)
-};
-
-inline CacheUnit cache_unit(const kvs_problem* p, int i) { return {(long long)p->in_row[i], (int)p->len[i], i}; }
-
-// The units of a launch.  Equal lengths at equal distances (the heads of a layer, or of all layers) follow from the first;
-// up to kInlineUnits others travel in the kernel arguments, more of them through the workspace.  Two types, because a
-// launch with a table in its arguments takes longer (see UnitTableT).
-struct EqualUnits {
-  long long in_row, step;
-  int len, first;
-  __device__ __forceinline__ CacheUnit unit(int i) const { return {in_row + i * step, len, first + i}; }
-};
-struct ListedUnits {
-  const CacheUnit* ext;   // DEVICE, or null: u
-  CacheUnit u[kInlineUnits];
-  __device__ __forceinline__ CacheUnit unit(int i) const {
-#if defined(__HIP_DEVICE_COMPILE__)
-    if (ext != nullptr) return ((const __attribute__((address_space(4))) CacheUnit*)ext)[i];
-#endif
-    return u[i];
-  }
-};
-
 // The cache of a launch.  Plain: k and v are rows of D values.  4 bits: k and v are codes (D / 2 bytes a row), ks and vs the
 // blocks' scales (D / 32 bytes a row).
 struct Cache {
@@ -92,9 +64,81 @@ __host__ __device__ inline int parts_of(int tiles, int part_tiles) {
   return tiles <= part_tiles ? 1 : (tiles + part_tiles - 1) / part_tiles;
 }
 
-// Partial results: [unit][query row in the order above][piece] of D numerators, the maximum and the denominator.
-__device__ __forceinline__ size_t part_at(const WindowShape& sh, int unit, int row, int piece) {
-  return (((size_t)unit * sh.R + row) * sh.n_parts + piece) * (size_t)(sh.D + 2);
+// Most tiles that a block of query rows of a unit of this length reaches (an upper bound of Reach::tiles), and the pieces that
+// the unit is given.
+inline int most_tiles(const WindowShape& sh, int len, int tile) {
+  auto tiles = [&](long long rows) { return (int)((rows + tile - 1) / tile); };
+  auto less = [](long long a, long long b) { return a < b ? a : b; };
+  if (sh.span == 0) return tiles(len);
+  const long long positions = sh.causal ? less(sh.W, (sh.block - 1) / sh.G + 2) : 1;
+  return tiles(less(len, sh.span + positions - 1)) + tiles(less(sh.sinks, len));
+}
+inline int unit_pieces(const WindowShape& sh, int len, int tile) { return parts_of(most_tiles(sh, len, tile), sh.part_tiles); }
+
+// One unit of a launch: its rows of the cache.
+struct CacheUnit {
+  long long in_row;
+  int len;
+  int index;            // position in the caller's problem (indexes Q and out)
+  int before;           // pieces of the problem's units before it (indexes partial results)
+};
+
+// The units of a launch.  Equal lengths at equal distances (the heads of a layer, or of all layers) follow from the first;
+// up to kInlineUnits others travel in the kernel arguments, more of them through the workspace.  Two types, because a
+// launch with a table in its arguments takes longer (see UnitTableT).
+struct EqualUnits {
+  static constexpr bool kListed = false;
+  long long in_row, step;
+  int len, first, n;
+  __device__ __forceinline__ CacheUnit unit(const WindowShape& sh, int i) const {
+    return {in_row + i * step, len, first + i, (first + i) * sh.n_parts};
+  }
+};
+struct UnitEntry {
+  long long in_row;
+  int len, before;
+};
+struct ListedUnits {
+  static constexpr bool kListed = true;
+  const UnitEntry* ext;   // DEVICE, or null: u
+  int first, n;           // position in the caller's problem of the first, and how many
+  int before, pieces;     // pieces of the units before them, and theirs
+  UnitEntry u[kInlineUnits];
+  __device__ __forceinline__ UnitEntry entry(int i) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if (ext != nullptr) return ((const __attribute__((address_space(4))) UnitEntry*)ext)[i];
+#endif
+    return u[i];
+  }
+  __device__ __forceinline__ CacheUnit unit(const WindowShape&, int i) const {
+    const UnitEntry e = entry(i);
+    return {e.in_row, e.len, first + i, e.before};
+  }
+  // The unit of piece f (0 <= f < pieces), by a search that looks at 64 units at once.  A grid as wide for every unit as the longest
+  // needs spends 2 ns on each workgroup that finds nothing to do (one token on 999 caches of 100 rows and one of 131072: 60 us, in
+  // such a grid 589).
+  __device__ __forceinline__ int unit_of(int f) const {
+    const int lane = threadIdx.x % kWave;
+    int lo = 0, count = n;
+    while (count > 1) {
+      const int step = (count + kWave - 1) / kWave, i = lane * step;
+      const bool not_after = i < count && (ext != nullptr ? ext[lo + i].before : u[lo + i].before) - before <= f;
+      const int k = __popcll(__ballot(not_after)) - 1;
+      lo += k * step;
+      count = min(step, count - k * step);
+    }
+    return lo;
+  }
+};
+
+// Pieces of all units of a launch.
+inline long long pieces_of(const EqualUnits& tab, const WindowShape& sh) { return (long long)tab.n * sh.n_parts; }
+inline long long pieces_of(const ListedUnits& tab, const WindowShape&) { return tab.pieces; }
+
+// Partial results: [piece, all units'][query row in the order above] of D numerators, the maximum and the denominator.  Where a
+// block's reach is one piece, its workgroup stores the output itself.
+__device__ __forceinline__ size_t part_at(const WindowShape& sh, const CacheUnit& un, int row, int piece) {
+  return ((size_t)(un.before + piece) * sh.R + row) * (size_t)(sh.D + 2);
 }
 // Where query row r of a unit is in Q and out, in rows of D.
 __device__ __forceinline__ size_t query_row(const WindowShape& sh, int unit, int r) {
@@ -127,17 +171,16 @@ __device__ __forceinline__ float quotient(float num, float den) { return den == 
 constexpr float kSlack = 8.f;
 
 // The launchers: `equal` or, where it is null, `listed`.
-hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                              CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
-                              hipStream_t stream);
+hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, CacheKind kind,
+                              const Cache& cache, const void* Q, void* out, float* part, hipStream_t stream);
 // bf16 outputs, blocks of 128 or 256 query rows (kvs_window_tiles.hip).
-hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                               CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
-                               hipStream_t stream);
-// out from the partial results of kernels whose tiles have `tile` rows (kWindowTile or kWideTile).
-hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                                bool f32, int tile, const float* part, void* out, hipStream_t stream);
+hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, CacheKind kind,
+                               const Cache& cache, const void* Q, void* out, float* part, hipStream_t stream);
+// out from the partial results of the units at, .., at + n - 1 of a launch of kernels whose tiles have `tile` rows (kWindowTile or
+// kWideTile).
+hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int at, int n, const WindowShape& sh, bool f32,
+                                int tile, const float* part, void* out, hipStream_t stream);
 // Descriptors of all units into the workspace.
-hipError_t launch_window_table(const kvs_problem* p, CacheUnit* dst, hipStream_t stream);
+hipError_t launch_window_table(const kvs_problem* p, const WindowShape& sh, int tile, UnitEntry* dst, hipStream_t stream);
 
 }  // namespace kvs

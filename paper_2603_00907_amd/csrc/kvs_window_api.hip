@@ -17,7 +17,7 @@ namespace {
 
 constexpr long long kMostRow = 1ll << 48;      // rows that a cache may have: byte offsets stay far below 2^63
 constexpr long long kComputeUnits = 256;
-constexpr long long kMostGroups = 1ll << 23;   // workgroups of one launch (a grid has less than 2^32 threads)
+constexpr long long kMostGroups = 1ll << 22;   // workgroups of one launch (a grid has less than 2^32 threads, a workgroup up to 768)
 
 // The fields that every one of these calls reads.
 kvs_status check_common(const kvs_problem* p, int* elt) {
@@ -55,16 +55,9 @@ struct WindowPlan {
   bool wide = false;           // kvs_window_tiles.hip, else kvs_window_rows.hip
   bool equal = false;          // units of one length at equal distances
   size_t part_bytes = 0, table_bytes = 0;
+  int tile() const { return wide ? kWideTile : kWindowTile; }
   size_t bytes() const { return part_bytes + table_bytes; }
 };
-
-// Most tiles that a block of query rows of a unit of this length reaches (an upper bound of Reach::tiles).
-long long tiles_bound(const WindowShape& sh, int len, int tile) {
-  auto tiles = [&](long long rows) { return (rows + tile - 1) / tile; };
-  if (sh.span == 0) return tiles(len);
-  const long long positions = sh.causal ? std::min<long long>(sh.W, (sh.block - 1) / sh.G + 2) : 1;
-  return tiles(std::min<long long>(len, sh.span + positions - 1)) + tiles(std::min(sh.sinks, len));
-}
 
 // How the rows that a block of query rows sees are cut into pieces, of at most kMaxParts.
 struct Cut {
@@ -75,26 +68,29 @@ struct Cut {
   bool equal = true;                             // reaches of one length
   Cut(const kvs_problem* problem, const WindowShape& shape, int rows) : p(problem), sh(shape), tile(rows) {
     for (int u = 0; u < p->n_units; ++u) {
-      most = std::max(most, tiles_bound(sh, p->len[u], tile));
+      most = std::max<long long>(most, most_tiles(sh, p->len[u], tile));
       equal = equal && p->len[u] == p->len[0];
     }
   }
-  // workgroups of a call whose pieces have `per` tiles at most; *tiles: those of all of them
-  long long workgroups(long long per, long long* tiles = nullptr) const {
-    long long n = 0, sum = 0, parts = 0, t = 0;
+  struct Sums { long long groups, tiles, partial; };   // workgroups, their tiles, workgroups that store partial results
+  // of a call whose pieces have `per` tiles at most
+  Sums with(long long per) const {
+    Sums s = {0, 0, 0};
+    long long parts = 0, t = 0;
     const int units = equal ? 1 : p->n_units;
     for (int u = 0; u < units; ++u) {
       if (u == 0 || p->len[u] != p->len[u - 1]) {
-        t = tiles_bound(sh, p->len[u], tile);
+        t = most_tiles(sh, p->len[u], tile);
         parts = std::max(1ll, (t + per - 1) / per);
       }
-      n += parts * sh.n_blocks;
-      sum += t * sh.n_blocks;
+      s.groups += parts;
+      s.tiles += t;
+      s.partial += parts > 1 ? parts : 0;
     }
-    const long long times = equal ? p->n_units : 1;
-    if (tiles) *tiles = sum * times;
-    return n * times;
+    const long long times = (equal ? p->n_units : 1ll) * sh.n_blocks;
+    return {s.groups * times, s.tiles * times, s.partial * times};
   }
+  long long workgroups(long long per) const { return with(per).groups; }
 };
 
 // kvs_window_rows.hip: the longest pieces that make no more workgroups than run at once, since memory bounds all of them alike and
@@ -131,7 +127,7 @@ void cut_rows(const kvs_problem* p, long long at_once, WindowShape& sh) {
 // kvs_window_tiles.hip, whose workgroups keep a compute unit busy by themselves and whose partial results are many: the number of
 // pieces with the shortest time, counted in tiles.  A workgroup takes kOnce tiles' time besides its tiles, and pieces cost a
 // launch that adds them up and their partials' way to memory and back.  (512 tokens of 32 heads on 8, 16 and 24 caches of 9000
-// rows: 95 us in four pieces, 173 in two (whole 265) and 268 whole; 24 of 2250 to 9000 245, whole 258, in the longest pieces of
+// rows: 95 us in four pieces, 173 in two (whole 265) and 268 whole; 24 of 2250 to 9000 218, whole 258, in the longest pieces of
 // at most 256 workgroups 378.)
 void cut_tiles(const kvs_problem* p, long long at_once, WindowShape& sh) {
   constexpr long long kOnce = 3;
@@ -141,12 +137,11 @@ void cut_tiles(const kvs_problem* p, long long at_once, WindowShape& sh) {
   // (1, 2, 3, 4, 6, 8, 12, 16, .. pieces)
   for (long long n = 1; n <= kMaxParts; n = n < 3 ? n + 1 : (n & (n - 1)) != 0 ? n / 3 * 4 : n / 2 * 3) {
     const long long per = std::max(4ll, (cut.most + n - 1) / n);
-    long long tiles = 0;
-    const long long groups = cut.workgroups(per, &tiles);
+    const auto [groups, tiles, partial] = cut.with(per);
     double time = cut.equal ? (double)((groups + at_once - 1) / at_once * (per + kOnce))
                             : (double)(tiles + groups * kOnce) / at_once + (double)(per + kOnce) / 2;
     if (n > 1) {
-      const double partials = 8.0 * p->n_units * sh.R * (sh.D + 2) * (double)((cut.most + per - 1) / per);
+      const double partials = 8.0 * std::min(sh.R, sh.block) * (sh.D + 2) * (double)partial;
       time += (kLaunchUs + partials / kBytesPerUs) / kTileUs;
     }
     if (n == 1 || time < best) {
@@ -202,9 +197,14 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
     plan->equal = plan->equal && p->len[u] == p->len[0] && p->in_row[u] - p->in_row[u - 1] == p->in_row[1] - p->in_row[0];
   }
   if (sh.n_parts > 1) {
-    plan->part_bytes = align_up((size_t)p->n_units * sh.R * sh.n_parts * (sh.D + 2) * sizeof(float));
+    long long pieces = (long long)p->n_units * sh.n_parts;
+    if (!plan->equal) {
+      pieces = 0;
+      for (int u = 0; u < p->n_units; ++u) pieces += unit_pieces(sh, p->len[u], plan->tile());
+    }
+    plan->part_bytes = align_up((size_t)pieces * sh.R * (sh.D + 2) * sizeof(float));
   }
-  if (!plan->equal && p->n_units > kInlineUnits) plan->table_bytes = align_up((size_t)p->n_units * sizeof(CacheUnit));
+  if (!plan->equal && p->n_units > kInlineUnits) plan->table_bytes = align_up((size_t)p->n_units * sizeof(UnitEntry));
   return KVS_OK;
 }
 
@@ -254,31 +254,51 @@ kvs_status window_attention(const kvs_problem* p, int32_t span, bool packed, con
   const hipStream_t s = (hipStream_t)hip_stream;
   (void)hipGetLastError();                     // an error left pending by the caller's earlier calls is not this call's
   float* part = sh.n_parts > 1 ? (float*)ws : nullptr;
-  const CacheUnit* table = nullptr;
+  UnitEntry* table = nullptr;
   hipError_t e = hipSuccess;
   if (plan.table_bytes > 0) {
-    CacheUnit* dst = (CacheUnit*)((char*)ws + plan.part_bytes);
-    table = dst;
-    e = launch_window_table(p, dst, s);
+    table = (UnitEntry*)((char*)ws + plan.part_bytes);
+    e = launch_window_table(p, sh, plan.tile(), table, s);
   }
   const CacheKind kind = elt == 4 ? (packed ? CacheKind::kPackedF32 : CacheKind::kF32)
                                   : (packed ? CacheKind::kPackedBf16 : CacheKind::kBf16);
   const auto launch = plan.wide ? launch_window_tiles : launch_window_rows;
   // (a call of more workgroups than a grid may have goes out in several launches)
-  const long long groups = std::max<long long>((long long)sh.n_blocks * sh.n_parts, sh.n_parts > 1 ? sh.R : 1);
-  const int most = (int)std::max<long long>(1, kMostGroups / groups);
-  for (int first = 0; e == hipSuccess && first < p->n_units; first += most) {
-    const int n = std::min(most, p->n_units - first);
+  const int most_units = (int)std::max<long long>(1, kMostGroups / (sh.n_parts > 1 ? sh.R : 1));
+  int before = 0;
+  for (int first = 0, n = 0; e == hipSuccess && first < p->n_units; first += n) {
+    EqualUnits equal;
+    ListedUnits listed;
+    int from = 0, to = 0;                      // units among these that are in pieces
     if (plan.equal) {
-      const long long step = p->n_units > 1 ? p->in_row[1] - p->in_row[0] : 0;
-      const EqualUnits units = {p->in_row[first], step, p->len[0], first};
-      e = launch(&units, nullptr, n, sh, kind, cache, Q, out, part, s);
+      n = (int)std::min<long long>({most_units, p->n_units - first,
+                                    std::max<long long>(1, kMostGroups / ((long long)sh.n_blocks * sh.n_parts))});
+      equal = {p->in_row[first], p->n_units > 1 ? p->in_row[1] - p->in_row[0] : 0, p->len[0], first, n};
+      to = sh.n_parts > 1 ? n : 0;
     } else {
-      ListedUnits units;
-      units.ext = table ? table + first : nullptr;
-      for (int i = 0; i < kInlineUnits; ++i) units.u[i] = cache_unit(p, first + std::min(i, n - 1));
-      e = launch(nullptr, &units, n, sh, kind, cache, Q, out, part, s);
+      listed.ext = table ? table + first : nullptr;
+      listed.first = first;
+      listed.before = before;
+      long long pieces = 0;
+      for (n = 0; n < most_units && first + n < p->n_units; ++n) {
+        const int mine = unit_pieces(sh, p->len[first + n], plan.tile());
+        if (n > 0 && (pieces + mine) * sh.n_blocks > kMostGroups) break;
+        if (!table) listed.u[n] = {p->in_row[first + n], p->len[first + n], before + (int)pieces};
+        if (mine > 1) {
+          if (to == 0) from = n;
+          to = n + 1;
+        }
+        pieces += mine;
+      }
+      for (int i = table ? 0 : n; i < kInlineUnits; ++i) listed.u[i] = UnitEntry{};
+      listed.n = n;
+      listed.pieces = (int)pieces;
+      before += (int)pieces;
     }
+    const EqualUnits* eq = plan.equal ? &equal : nullptr;
+    const ListedUnits* li = plan.equal ? nullptr : &listed;
+    e = launch(eq, li, sh, kind, cache, Q, out, part, s);
+    if (e == hipSuccess && to > from) e = launch_window_reduce(eq, li, from, to - from, sh, elt == 4, plan.tile(), part, out, s);
   }
   return launched(e, "an attention launch");
 }

@@ -39,7 +39,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kTile = kWindowTile;
 constexpr int kReduceThreads = 256;
 
-// A piece of a unit's rows (at most 2^31 bytes of them): one scalar base, 32-bit offsets.
+// Of a tile: one base, the same for all lanes, and 32-bit offsets.
 template <typename T>
 __device__ __forceinline__ T at(const char* base, uint32_t offset) { return *(const T*)(base + offset); }
 
@@ -272,11 +272,26 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, NQ>())) voi
   __shared__ __attribute__((aligned(16))) float sm_acc[WAVES][16][ACCW];
 
   const int id = blockIdx.x;
-  const int piece = id % sh.n_parts, block = id / sh.n_parts % sh.n_blocks;
-  const CacheUnit un = tab.unit(id / sh.n_parts / sh.n_blocks);
+  int piece = 0, block, at_unit;
+  if (Tab::kListed || sh.n_parts == 1) {
+    block = id % sh.n_blocks;
+    at_unit = id / sh.n_blocks;
+    if constexpr (Tab::kListed) {
+      if (sh.n_parts > 1) {
+        piece = at_unit + tab.before;
+        at_unit = tab.unit_of(at_unit);
+        piece -= tab.entry(at_unit).before;
+      }
+    }
+  } else {
+    piece = id % sh.n_parts;
+    block = id / sh.n_parts % sh.n_blocks;
+    at_unit = id / sh.n_parts / sh.n_blocks;
+  }
+  const CacheUnit un = tab.unit(sh, at_unit);
   const Reach re = reach_of<kTile>(sh, un.len, block);
   const int n_parts = parts_of(re.tiles, sh.part_tiles);
-  if (piece >= n_parts) return;             // the grid is as wide as the longest reach needs
+  if (piece >= n_parts) return;             // (a block whose reach is shorter than others of the unit)
   const int tile1 = min(re.tiles, (piece + 1) * sh.part_tiles);
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
   const int c = lane % 16, g = lane / 16;
@@ -535,10 +550,10 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, NQ>())) voi
           den_q = fmaf(lw, wgt, den_q);
         }
       }
-      if (sh.n_parts == 1) {
+      if (n_parts == 1) {
         store_two((Io*)out + query_row(sh, un.index, row) * D + ch, quotient(a, den_q), quotient(b, den_q));
       } else {
-        float* dst = part + part_at(sh, un.index, row, piece);
+        float* dst = part + part_at(sh, un, row, piece);
         *(float2*)(dst + ch) = make_float2(a, b);
         if (ch == 0) { dst[D] = M; dst[D + 1] = den_q; }
       }
@@ -549,26 +564,29 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, NQ>())) voi
 // out[row] from its pieces, in order.  One workgroup per (unit, query row): thread (g, d) adds up every PARTS-th piece of
 // channel d, and the sums are added in order.
 template <typename Io, int D, int TILE, typename Tab>
-__global__ __launch_bounds__(kReduceThreads) void window_reduce_kernel(const Tab tab, const WindowShape sh,
-                                                                 const float* __restrict__ part, void* __restrict__ out) {
+__global__ __launch_bounds__(kReduceThreads) void window_reduce_kernel(const Tab tab, const WindowShape sh, int unit0,
+                                                                       const float* __restrict__ part,
+                                                                       void* __restrict__ out) {
   constexpr int PARTS = kReduceThreads / D;
   __shared__ float sm_w[kMaxParts];
   __shared__ float sm_num[PARTS][D];
-  __shared__ float sm_top[(kReduceThreads / kWave)], sm_den[(kReduceThreads / kWave)];
-  const CacheUnit un = tab.unit(blockIdx.x / sh.R);
+  __shared__ float sm_top[kReduceThreads / kWave], sm_den[kReduceThreads / kWave];
+  const CacheUnit un = tab.unit(sh, unit0 + blockIdx.x / sh.R);
   const int row = blockIdx.x % sh.R;
   const int n = parts_of(reach_of<TILE>(sh, un.len, row / sh.block).tiles, sh.part_tiles);
-  const float* src = part + part_at(sh, un.index, row, 0);
+  if (n == 1) return;                      // (stored already)
+  const float* src = part + part_at(sh, un, row, 0);
+  const size_t step = (size_t)sh.R * (D + 2);
   const int tid = threadIdx.x, d = tid % D, g = tid / D;
-  const float m = tid < n ? src[(size_t)tid * (D + 2) + D] : -INFINITY;
-  const float l = tid < n ? src[(size_t)tid * (D + 2) + D + 1] : 0.f;
+  const float m = tid < n ? src[tid * step + D] : -INFINITY;
+  const float l = tid < n ? src[tid * step + D + 1] : 0.f;
   float M = m;
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor(M, k, kWave));
   if (tid % kWave == 0) sm_top[tid / kWave] = M;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < (kReduceThreads / kWave); ++w) M = fmaxf(M, sm_top[w]);
+  for (int w = 0; w < kReduceThreads / kWave; ++w) M = fmaxf(M, sm_top[w]);
   const float wgt = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M);
   if (tid < n) sm_w[tid] = wgt;
   float den = l == 0.f ? 0.f : l * wgt;
@@ -580,7 +598,7 @@ __global__ __launch_bounds__(kReduceThreads) void window_reduce_kernel(const Tab
   for (int i0 = g; i0 < n; i0 += 8 * PARTS) {                // eight loads at a time
     float x[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) x[u] = src[(size_t)min(i0 + u * PARTS, n - 1) * (D + 2) + d];
+    for (int u = 0; u < 8; ++u) x[u] = src[min(i0 + u * PARTS, n - 1) * step + d];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       if (i0 + u * PARTS < n) num = fmaf(x[u], sm_w[i0 + u * PARTS], num);
@@ -593,7 +611,7 @@ __global__ __launch_bounds__(kReduceThreads) void window_reduce_kernel(const Tab
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) { a += sm_num[i][2 * tid]; b += sm_num[i][2 * tid + 1]; }
 #pragma unroll
-    for (int w = 0; w < (kReduceThreads / kWave); ++w) total += sm_den[w];
+    for (int w = 0; w < kReduceThreads / kWave; ++w) total += sm_den[w];
     store_two((Io*)out + query_row(sh, un.index, row) * D + 2 * tid, quotient(a, total), quotient(b, total));
   }
 }
@@ -602,20 +620,22 @@ __global__ __launch_bounds__(kReduceThreads) void window_reduce_kernel(const Tab
 // once, so that the partials cost one round trip and nobody meets.
 constexpr int kFewParts = 8;
 template <typename Io, int D, int TILE, typename Tab>
-__global__ __launch_bounds__(kReduceThreads) void window_reduce_few_kernel(const Tab tab, const WindowShape sh, int n_rows,
+__global__ __launch_bounds__(kReduceThreads) void window_reduce_few_kernel(const Tab tab, const WindowShape sh, int unit0,
+                                                                           int n_rows,
                                                                            const float* __restrict__ part,
                                                                            void* __restrict__ out) {
   constexpr int PER = D / 2;               // threads per row
   const int at = (int)blockIdx.x * (kReduceThreads / PER) + (int)threadIdx.x / PER, ch = (int)threadIdx.x % PER * 2;
   if (at >= n_rows) return;
-  const CacheUnit un = tab.unit(at / sh.R);
+  const CacheUnit un = tab.unit(sh, unit0 + at / sh.R);
   const int row = at % sh.R;
   const int n = parts_of(reach_of<TILE>(sh, un.len, row / sh.block).tiles, sh.part_tiles);
-  const float* src = part + part_at(sh, un.index, row, 0);
+  if (n == 1) return;                      // (stored already)
+  const float* src = part + part_at(sh, un, row, 0);
   float2 x[kFewParts], ml[kFewParts];
 #pragma unroll
   for (int i = 0; i < kFewParts; ++i) {
-    const float* p = src + min(i, n - 1) * (D + 2);
+    const float* p = src + (size_t)min(i, n - 1) * sh.R * (D + 2);
     x[i] = *(const float2*)(p + ch);
     ml[i] = *(const float2*)(p + D);
   }
@@ -637,16 +657,16 @@ __global__ __launch_bounds__(kReduceThreads) void window_reduce_few_kernel(const
 
 // Unit descriptors of a launch that has too many for its arguments, stored by a kernel that carries some in its own.
 constexpr int kTableBatch = 224;
-struct CacheUnitBatch { CacheUnit u[kTableBatch]; };
-__global__ __launch_bounds__(256) void cache_unit_table_kernel(const CacheUnitBatch batch, int n, CacheUnit* __restrict__ dst) {
+struct UnitBatch { UnitEntry u[kTableBatch]; };
+__global__ __launch_bounds__(256) void unit_table_kernel(const UnitBatch batch, int n, UnitEntry* __restrict__ dst) {
   const int i = threadIdx.x;
   if (i < n) dst[i] = batch.u[i];
 }
 
 template <CacheKind KIND, int D, typename Tab>
-hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
-                       float* part, hipStream_t stream) {
-  const dim3 grid((unsigned)((long long)n_units * sh.n_blocks * sh.n_parts));
+hipError_t launch_kind(const Tab& tab, const WindowShape& sh, const Cache& cache, const void* Q, void* out, float* part,
+                       hipStream_t stream) {
+  const dim3 grid((unsigned)(pieces_of(tab, sh) * sh.n_blocks));
   auto go = [&](auto nq, auto waves) {
     constexpr int NQ = decltype(nq)::value, WAVES = decltype(waves)::value;
     auto counted = [&](auto counts) {
@@ -667,47 +687,43 @@ hipError_t launch_kind(const Tab& tab, int n_units, const WindowShape& sh, const
 }
 
 template <CacheKind KIND, typename Tab>
-hipError_t launch_d(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
-                    float* part, hipStream_t stream) {
-  return sh.D == 64 ? launch_kind<KIND, 64>(tab, n_units, sh, cache, Q, out, part, stream)
-                    : launch_kind<KIND, 128>(tab, n_units, sh, cache, Q, out, part, stream);
+hipError_t launch_d(const Tab& tab, const WindowShape& sh, const Cache& cache, const void* Q, void* out, float* part,
+                    hipStream_t stream) {
+  return sh.D == 64 ? launch_kind<KIND, 64>(tab, sh, cache, Q, out, part, stream)
+                    : launch_kind<KIND, 128>(tab, sh, cache, Q, out, part, stream);
 }
 
 template <typename Tab>
-hipError_t launch_tab(const Tab& tab, int n_units, const WindowShape& sh, CacheKind kind, const Cache& cache,
-                      const void* Q, void* out, float* part, hipStream_t stream) {
+hipError_t launch_tab(const Tab& tab, const WindowShape& sh, CacheKind kind, const Cache& cache, const void* Q, void* out,
+                      float* part, hipStream_t stream) {
   switch (kind) {
-    case CacheKind::kF32: return launch_d<CacheKind::kF32>(tab, n_units, sh, cache, Q, out, part, stream);
-    case CacheKind::kBf16: return launch_d<CacheKind::kBf16>(tab, n_units, sh, cache, Q, out, part, stream);
-    case CacheKind::kPackedF32: return launch_d<CacheKind::kPackedF32>(tab, n_units, sh, cache, Q, out, part, stream);
-    default: return launch_d<CacheKind::kPackedBf16>(tab, n_units, sh, cache, Q, out, part, stream);
+    case CacheKind::kF32: return launch_d<CacheKind::kF32>(tab, sh, cache, Q, out, part, stream);
+    case CacheKind::kBf16: return launch_d<CacheKind::kBf16>(tab, sh, cache, Q, out, part, stream);
+    case CacheKind::kPackedF32: return launch_d<CacheKind::kPackedF32>(tab, sh, cache, Q, out, part, stream);
+    default: return launch_d<CacheKind::kPackedBf16>(tab, sh, cache, Q, out, part, stream);
   }
 }
 
 }  // namespace
 
-hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                              CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
-                              hipStream_t stream) {
-  const hipError_t e = equal ? launch_tab(*equal, n_units, sh, kind, cache, Q, out, part, stream)
-                             : launch_tab(*listed, n_units, sh, kind, cache, Q, out, part, stream);
-  if (e != hipSuccess || sh.n_parts == 1) return e;
-  const bool f32 = kind == CacheKind::kF32 || kind == CacheKind::kPackedF32;
-  return launch_window_reduce(equal, listed, n_units, sh, f32, kTile, part, out, stream);
+hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, CacheKind kind,
+                              const Cache& cache, const void* Q, void* out, float* part, hipStream_t stream) {
+  return equal ? launch_tab(*equal, sh, kind, cache, Q, out, part, stream)
+               : launch_tab(*listed, sh, kind, cache, Q, out, part, stream);
 }
 
-hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                                bool f32, int tile, const float* part, void* out, hipStream_t stream) {
-  const int rows = n_units * sh.R;
+hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int at, int n, const WindowShape& sh, bool f32,
+                                int tile, const float* part, void* out, hipStream_t stream) {
+  const int rows = n * sh.R;
   auto go = [&](const auto& tab, auto io, auto d, auto t) {
     constexpr int D = decltype(d)::value, TILE = decltype(t)::value, PER = kReduceThreads / (D / 2);
     typedef std::decay_t<decltype(tab)> Tab;
     if (sh.n_parts <= kFewParts) {
       hipLaunchKernelGGL((window_reduce_few_kernel<decltype(io), D, TILE, Tab>), dim3((rows + PER - 1) / PER),
-                         dim3(kReduceThreads), 0, stream, tab, sh, rows, part, out);
+                         dim3(kReduceThreads), 0, stream, tab, sh, at, rows, part, out);
     } else {
       hipLaunchKernelGGL((window_reduce_kernel<decltype(io), D, TILE, Tab>), dim3(rows), dim3(kReduceThreads), 0, stream, tab,
-                         sh, part, out);
+                         sh, at, part, out);
     }
   };
   auto typed = [&](const auto& tab, auto d) {
@@ -724,12 +740,16 @@ hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* list
   return hipGetLastError();
 }
 
-hipError_t launch_window_table(const kvs_problem* p, CacheUnit* dst, hipStream_t stream) {
+hipError_t launch_window_table(const kvs_problem* p, const WindowShape& sh, int tile, UnitEntry* dst, hipStream_t stream) {
+  int before = 0;
   for (int at = 0; at < p->n_units; at += kTableBatch) {
     const int n = p->n_units - at < kTableBatch ? p->n_units - at : kTableBatch;
-    CacheUnitBatch batch;
-    for (int i = 0; i < kTableBatch; ++i) batch.u[i] = cache_unit(p, at + (i < n ? i : 0));
-    hipLaunchKernelGGL(cache_unit_table_kernel, dim3(1), dim3(256), 0, stream, batch, n, dst + at);
+    UnitBatch batch = {};
+    for (int i = 0; i < n; ++i) {
+      batch.u[i] = {(long long)p->in_row[at + i], (int)p->len[at + i], before};
+      before += unit_pieces(sh, p->len[at + i], tile);
+    }
+    hipLaunchKernelGGL(unit_table_kernel, dim3(1), dim3(256), 0, stream, batch, n, dst + at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

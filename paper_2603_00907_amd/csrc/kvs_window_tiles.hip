@@ -34,8 +34,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = kWideTile;
-// A lane's sixteen terms may add up to this before their reference is raised to the largest logit.
-constexpr float kMostSum = 1024.f;
+// A lane's sixteen terms may add up to this before their reference is raised to the largest logit: sixteen logits that are equal,
+// of slots with up to 4096 copies (512 tokens of 32 heads on 32 caches of 2560 slots, 1 to 200 copies, logits close together: 93 us,
+// with 1024 130).
+constexpr float kMostSum = 65536.f;
 
 // Where piece `p` (16 bytes) of row r is within its row.
 template <int D> __device__ __forceinline__ int key_slot(int r, int p) { return D == 128 ? p ^ (r % 16) : p ^ (r / 2 % 8); }
@@ -104,7 +106,7 @@ constexpr int waves_per_simd() {
 
 template <CacheKind KIND, int D, int WAVES, bool COUNTS, typename Tab>
 __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, WAVES, COUNTS>())) void window_tiles_kernel(
-    const Tab tab, const WindowShape sh, const Cache cache, int n_units, const uint16_t* __restrict__ Q,
+    const Tab tab, const WindowShape sh, const Cache cache, int width, const uint16_t* __restrict__ Q,
     uint16_t* __restrict__ out, float* __restrict__ part) {
   constexpr int kThreads = WAVES * kWave;
   constexpr int KS = D / 16;                // steps of the contraction over channels
@@ -115,14 +117,27 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, WAVES, COUN
   // cardinalities as pairs hi + lo of bf16 numbers (exact up to 65536, to 2^-16 beyond): of four rows both hi pairs, then both lo
   __shared__ u32x4 sm_cnt[2][kTile / 4];
 
-  // A unit's workgroups are n_units apart, which puts them on one XCD where n_units is a multiple of eight, and the last
-  // blocks, which see most under a causal mask, come first.
+  // Workgroups on the same rows are `width` apart, which puts them on one XCD where it is a multiple of eight (as it is of listed
+  // units), and the last blocks, which see most under a causal mask, come first.  Pieces of one unit are spread over the XCDs (512
+  // tokens on 31 caches of 100 rows and one of 131072: 194 us, with all of a unit's on one 3812).
   const int id = blockIdx.x;
-  const int piece = id / n_units % sh.n_parts;
-  const int block = sh.n_blocks - 1 - id / n_units / sh.n_parts;
-  const CacheUnit un = tab.unit(id % n_units);
+  int at_unit = id % width, piece = 0, block = id / width;
+  if constexpr (Tab::kListed) {
+    if (at_unit >= tab.pieces) return;
+    if (sh.n_parts > 1) {
+      piece = at_unit + tab.before;
+      at_unit = tab.unit_of(at_unit);
+      piece -= tab.entry(at_unit).before;
+    }
+  } else {
+    piece = block % sh.n_parts;
+    block /= sh.n_parts;
+  }
+  block = sh.n_blocks - 1 - block;
+  const CacheUnit un = tab.unit(sh, at_unit);
   const Reach re = reach_of<kTile>(sh, un.len, block);
-  if (piece >= parts_of(re.tiles, sh.part_tiles)) return;     // the grid is as wide as the longest reach needs
+  const int n_parts = parts_of(re.tiles, sh.part_tiles);
+  if (piece >= n_parts) return;             // (a block whose reach is shorter than others of the unit)
   const int j0 = piece * sh.part_tiles, j1 = min(re.tiles, j0 + sh.part_tiles);
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
   const int col = lane % 32, half = lane / 32;
@@ -350,7 +365,7 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, WAVES, COUN
   // element v of block d: channel 32 d + 8 (v / 4) + 4 half + v % 4 of the lane's query
   const float den = l + __shfl_xor(l, 32, kWave);
   if (row >= sh.R) return;
-  if (sh.n_parts == 1) {
+  if (n_parts == 1) {
     uint16_t* dst = out + query_row(sh, un.index, row) * D + 4 * half;
     const float inv = quotient(1.f, den);
 #pragma unroll
@@ -362,7 +377,7 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, WAVES, COUN
       }
     }
   } else {
-    float* dst = part + part_at(sh, un.index, row, piece);
+    float* dst = part + part_at(sh, un, row, piece);
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
 #pragma unroll
@@ -376,39 +391,38 @@ __global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, WAVES, COUN
 }
 
 template <CacheKind KIND, int D, int WAVES, typename Tab>
-hipError_t launch_waves(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
-                     float* part, hipStream_t stream) {
-  const dim3 grid((unsigned)((long long)n_units * sh.n_blocks * sh.n_parts));
+hipError_t launch_waves(const Tab& tab, const WindowShape& sh, const Cache& cache, const void* Q, void* out, float* part,
+                        hipStream_t stream) {
+  const long long pieces = pieces_of(tab, sh);
+  const int width = Tab::kListed ? (int)((pieces + 7) / 8 * 8) : tab.n;
+  const dim3 grid((unsigned)((Tab::kListed ? width : pieces) * sh.n_blocks));
   if (cache.counts) {
-    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, WAVES, true, Tab>), grid, dim3(WAVES * kWave), 0, stream, tab, sh, cache, n_units,
+    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, WAVES, true, Tab>), grid, dim3(WAVES * kWave), 0, stream, tab, sh, cache, width,
                        (const uint16_t*)Q, (uint16_t*)out, part);
   } else {
-    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, WAVES, false, Tab>), grid, dim3(WAVES * kWave), 0, stream, tab, sh, cache, n_units,
+    hipLaunchKernelGGL((window_tiles_kernel<KIND, D, WAVES, false, Tab>), grid, dim3(WAVES * kWave), 0, stream, tab, sh, cache, width,
                        (const uint16_t*)Q, (uint16_t*)out, part);
   }
   return hipGetLastError();
 }
 
 template <CacheKind KIND, typename Tab>
-hipError_t launch_sized(const Tab& tab, int n_units, const WindowShape& sh, const Cache& cache, const void* Q, void* out,
-                        float* part, hipStream_t stream) {
-  if (sh.D == 64) return launch_waves<KIND, 64, 4>(tab, n_units, sh, cache, Q, out, part, stream);
-  return sh.block == 128 ? launch_waves<KIND, 128, 4>(tab, n_units, sh, cache, Q, out, part, stream)
-                         : launch_waves<KIND, 128, 8>(tab, n_units, sh, cache, Q, out, part, stream);
+hipError_t launch_sized(const Tab& tab, const WindowShape& sh, const Cache& cache, const void* Q, void* out, float* part,
+                        hipStream_t stream) {
+  if (sh.D == 64) return launch_waves<KIND, 64, 4>(tab, sh, cache, Q, out, part, stream);
+  return sh.block == 128 ? launch_waves<KIND, 128, 4>(tab, sh, cache, Q, out, part, stream)
+                         : launch_waves<KIND, 128, 8>(tab, sh, cache, Q, out, part, stream);
 }
 
 }  // namespace
 
-hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                               CacheKind kind, const Cache& cache, const void* Q, void* out, float* part,
-                               hipStream_t stream) {
+hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, CacheKind kind,
+                               const Cache& cache, const void* Q, void* out, float* part, hipStream_t stream) {
   auto go = [&](const auto& tab) {
-    return kind == CacheKind::kBf16 ? launch_sized<CacheKind::kBf16>(tab, n_units, sh, cache, Q, out, part, stream)
-                                    : launch_sized<CacheKind::kPackedBf16>(tab, n_units, sh, cache, Q, out, part, stream);
+    return kind == CacheKind::kBf16 ? launch_sized<CacheKind::kBf16>(tab, sh, cache, Q, out, part, stream)
+                                    : launch_sized<CacheKind::kPackedBf16>(tab, sh, cache, Q, out, part, stream);
   };
-  const hipError_t e = equal ? go(*equal) : go(*listed);
-  if (e != hipSuccess || sh.n_parts == 1) return e;
-  return launch_window_reduce(equal, listed, n_units, sh, false, kTile, part, out, stream);
+  return equal ? go(*equal) : go(*listed);
 }
 
 }  // namespace kvs

@@ -23,58 +23,90 @@ const kvs_problem* g_problem = nullptr;   // the call under way
 size_t g_ws_bytes = 0;
 char* g_ws = nullptr;
 std::vector<int> g_done;                  // units launched
-std::vector<kvs::CacheUnit> g_table;
+std::vector<kvs::UnitEntry> g_table;
+long long g_before = 0;                   // pieces of the units launched
+size_t g_reduced = 0;                     // units whose partial results have been added up
 }  // namespace
 
 namespace kvs {
 
 int debug_switch(kvs_debug_switch) { return 0; }
 
-hipError_t launch_window_table(const kvs_problem* p, CacheUnit* dst, hipStream_t) {
+hipError_t launch_window_table(const kvs_problem* p, const WindowShape& sh, int tile, UnitEntry* dst, hipStream_t) {
   CHECK((char*)dst >= g_ws && (char*)(dst + p->n_units) <= g_ws + g_ws_bytes);
   g_table.clear();
-  for (int i = 0; i < p->n_units; ++i) g_table.push_back(cache_unit(p, i));
-  return hipSuccess;
-}
-
-template <int TILE>
-hipError_t attended(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh, float* part) {
-  CHECK((equal != nullptr) != (listed != nullptr));
-  CHECK(n_units > 0 && (listed == nullptr || listed->ext != nullptr || n_units <= kInlineUnits));
-  CHECK((long long)n_units * sh.n_blocks * sh.n_parts < 1ll << 24);
-  CHECK(sh.n_parts <= kMaxParts && (long long)sh.n_blocks * sh.block >= sh.R && sh.block <= 256);
-  CHECK(sh.n_parts == 1 || (long long)n_units * sh.R < 1ll << 24);
-  for (int i = 0; i < n_units; ++i) {
-    CacheUnit un;
-    if (equal) un = {equal->in_row + i * equal->step, equal->len, equal->first + i};
-    else if (listed->ext) un = g_table[(size_t)(g_done.size())];
-    else un = listed->u[i];
-    g_done.push_back(un.index);
-    CHECK(un.len == g_problem->len[un.index] && un.in_row == g_problem->in_row[un.index]);
-    for (int b = 0; b < sh.n_blocks; b += 1 + sh.n_blocks / 20) {
-      const Reach r = reach_of<TILE>(sh, un.len, b);
-      CHECK(parts_of(r.tiles, sh.part_tiles) <= sh.n_parts);
-      CHECK(0 <= r.sink_end && r.sink_end <= r.first && r.first <= r.end && r.end <= un.len);
-      CHECK(r.sink_tiles * TILE >= r.sink_end && (r.tiles - r.sink_tiles) * TILE >= r.end - r.first);
-    }
-    if (sh.n_parts > 1) {
-      const size_t last = (((size_t)un.index * sh.R + sh.R - 1) * sh.n_parts + sh.n_parts - 1) * (sh.D + 2) + sh.D + 2;
-      CHECK((char*)part >= g_ws && (char*)(part + last) <= g_ws + g_ws_bytes);
-      CHECK(g_table.empty() || listed == nullptr || listed->ext == nullptr || (char*)(part + last) <= (char*)listed->ext);
-    }
+  int before = 0;
+  for (int i = 0; i < p->n_units; ++i) {
+    g_table.push_back({p->in_row[i], p->len[i], before});
+    before += unit_pieces(sh, p->len[i], tile);
   }
   return hipSuccess;
 }
-hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                              CacheKind, const Cache&, const void*, void*, float* part, hipStream_t) {
-  CHECK(sh.block == 16 || sh.block == 32);
-  return attended<kWindowTile>(equal, listed, n_units, sh, part);
+
+// A unit of the launch, as its kernels see it.
+CacheUnit unit_at(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, int i) {
+  if (equal) return {equal->in_row + i * equal->step, equal->len, equal->first + i, (equal->first + i) * sh.n_parts};
+  const UnitEntry e = listed->ext ? g_table[listed->first + i] : listed->u[i];
+  return {e.in_row, e.len, listed->first + i, e.before};
 }
-hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, int n_units, const WindowShape& sh,
-                               CacheKind kind, const Cache&, const void*, void*, float* part, hipStream_t) {
+
+template <int TILE>
+hipError_t attended(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, float* part) {
+  CHECK((equal != nullptr) != (listed != nullptr));
+  const int n_units = equal ? equal->n : listed->n, first = equal ? equal->first : listed->first;
+  const long long pieces = equal ? pieces_of(*equal, sh) : pieces_of(*listed, sh);
+  CHECK(n_units > 0 && first == (int)g_done.size() && (listed == nullptr || listed->ext != nullptr || n_units <= kInlineUnits));
+  CHECK(pieces >= n_units && pieces * sh.n_blocks < 1ll << 24);
+  CHECK(sh.n_parts <= kMaxParts && (long long)sh.n_blocks * sh.block >= sh.R && sh.block <= 256);
+  CHECK(listed == nullptr || listed->before == g_before);
+  g_reduced = std::max(g_reduced, g_done.size());
+  for (int i = 0; i < n_units; ++i) {
+    const CacheUnit un = unit_at(equal, listed, sh, i);
+    g_done.push_back(un.index);
+    CHECK(un.len == g_problem->len[un.index] && un.in_row == g_problem->in_row[un.index]);
+    CHECK(un.before == g_before);
+    const int mine = unit_pieces(sh, un.len, TILE);
+    CHECK(mine >= 1 && mine <= sh.n_parts);
+    g_before += equal ? sh.n_parts : mine;
+    for (int b = 0; b < sh.n_blocks; b += 1 + sh.n_blocks / 20) {
+      const Reach r = reach_of<TILE>(sh, un.len, b);
+      CHECK(parts_of(r.tiles, sh.part_tiles) <= mine);
+      CHECK(0 <= r.sink_end && r.sink_end <= r.first && r.first <= r.end && r.end <= un.len);
+      CHECK(r.sink_tiles * TILE >= r.sink_end && (r.tiles - r.sink_tiles) * TILE >= r.end - r.first);
+    }
+    if (mine > 1) {
+      const size_t last = ((size_t)(un.before + mine - 1) * sh.R + sh.R - 1) * (sh.D + 2) + sh.D + 2;
+      CHECK((char*)part >= g_ws && (char*)(part + last) <= g_ws + g_ws_bytes);
+      // (the table lies behind the partial results)
+      CHECK(listed == nullptr || listed->ext == nullptr || (char*)(part + last) <= (char*)(listed->ext - listed->first));
+    }
+  }
+  if (listed) CHECK(g_before - listed->before == listed->pieces);
+  return hipSuccess;
+}
+hipError_t launch_window_rows(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, CacheKind, const Cache&,
+                              const void*, void*, float* part, hipStream_t) {
+  CHECK(sh.block == 16 || sh.block == 32);
+  return attended<kWindowTile>(equal, listed, sh, part);
+}
+hipError_t launch_window_tiles(const EqualUnits* equal, const ListedUnits* listed, const WindowShape& sh, CacheKind kind,
+                               const Cache&, const void*, void*, float* part, hipStream_t) {
   CHECK(sh.block == 128 || sh.block == 256);
   CHECK(kind == CacheKind::kBf16 || kind == CacheKind::kPackedBf16);
-  return attended<kWideTile>(equal, listed, n_units, sh, part);
+  return attended<kWideTile>(equal, listed, sh, part);
+}
+hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* listed, int at, int n, const WindowShape& sh, bool,
+                                int tile, const float* part, void*, hipStream_t) {
+  const int n_units = equal ? equal->n : listed->n;
+  CHECK(part != nullptr && sh.n_parts > 1 && n > 0 && at >= 0 && at + n <= n_units && (long long)n * sh.R < 1ll << 24);
+  // every unit in pieces is among them
+  const size_t first = g_done.size() - n_units;
+  CHECK(g_reduced <= first);
+  for (int i = 0; i < n_units; ++i) {
+    CHECK((i >= at && i < at + n) || unit_pieces(sh, unit_at(equal, listed, sh, i).len, tile) == 1);
+  }
+  g_reduced = g_done.size();
+  return hipSuccess;
 }
 
 namespace {
@@ -128,7 +160,7 @@ kvs_status attend(const Call& c, int span, bool packed) {
   kvs_status st = kvs_window_attention_workspace_size(&c.p, span, &bytes);
   if (st != KVS_OK) return st;
   CHECK(bytes % 256 == 0);
-  g_problem = &c.p; g_ws = (char*)at(9); g_ws_bytes = bytes; g_done.clear(); g_table.clear();
+  g_problem = &c.p; g_ws = (char*)at(9); g_ws_bytes = bytes; g_done.clear(); g_table.clear(); g_before = 0; g_reduced = 0;
   if (bytes > 0) {
     auto with = [&](void* ws, size_t n) {
       return kvs_window_attention(&c.p, span, at(0), at(1), at(2), nullptr, at(3), ws, n, nullptr);
@@ -143,6 +175,7 @@ kvs_status attend(const Call& c, int span, bool packed) {
   if (st == KVS_OK) {
     CHECK((int)g_done.size() == c.p.n_units);
     for (int i = 0; i < c.p.n_units; ++i) CHECK(g_done[i] == i);
+    CHECK(g_before == c.p.n_units || g_reduced > 0);     // (more pieces than units: they have been added up)
   }
   return st;
 }
@@ -180,6 +213,16 @@ int main() {
     }
     CHECK(convert(c) == KVS_OK);
   }
+  // one long unit among many: its pieces are no reason for a large workspace
+  for (int units : {50, 20000}) {
+    std::vector<int32_t> lens(units, 100);
+    lens[units / 2] = 1000000;
+    Call c(lens);
+    size_t bytes = 0;
+    CHECK(attend(c, 0, false) == KVS_OK);
+    CHECK(kvs_window_attention_workspace_size(&c.p, 0, &bytes) == KVS_OK);
+    CHECK(bytes > 0 && bytes <= (units + 3 * 256ull) * (4 * 130 * 4 + 16) + 512);
+  }
   // the largest calls
   CHECK(attend(Call({KVS_MAX_LEN}, 1, KVS_MAX_WINDOW_ROWS), 0, false) == KVS_OK);
   CHECK(attend(Call({KVS_MAX_LEN, 1, 0}, 64, 65536), 2147483647, true) == KVS_OK);
@@ -215,7 +258,7 @@ int main() {
   CHECK(kvs_window_attention_workspace_size(nullptr, 0, &bytes) == KVS_ERR_INVALID_ARG);
   Call c({10, 20});
   CHECK(kvs_window_attention_workspace_size(&c.p, 0, nullptr) == KVS_ERR_INVALID_ARG);
-  g_problem = &c.p; g_done.clear();
+  g_problem = &c.p; g_done.clear(); g_before = 0; g_reduced = 0;
   auto win = [&](void* q, void* k, void* v, void* n, void* o) {
     return kvs_window_attention(&c.p, 0, q, k, v, (const int32_t*)n, o, nullptr, 0, nullptr);
   };
@@ -255,7 +298,7 @@ int main() {
   CHECK(pack(at(0), at(1), at(2), at(3), at(4), at(5)) == KVS_ERR_INVALID_ARG);
   // units of no rows need no buffers of rows
   Call none({0, 0});
-  g_problem = &none.p; g_done.clear();
+  g_problem = &none.p; g_done.clear(); g_before = 0; g_reduced = 0;
   CHECK(kvs_window_attention(&none.p, 0, at(0), nullptr, nullptr, nullptr, at(3), nullptr, 0, nullptr) == KVS_OK);
   CHECK(g_done.size() == 2);
   CHECK(kvs_pack(&none.p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr) == KVS_OK && g_done.size() == 2);

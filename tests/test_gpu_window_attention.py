@@ -130,6 +130,15 @@ def test_many_units_equal_and_not(dtype, packed):
 
 
 @pytest.mark.parametrize("dtype,packed", CACHES)
+@pytest.mark.parametrize("lens,G,W", [([100] * 40 + [20000, 0, 70], 4, 1), ([33] * 300 + [30000] + [20] * 100, 4, 1),
+                                      ([30000] + [2] * 4500 + [9000, 1], 1, 1), ([60] * 20 + [12000] + [60] * 3, 4, 20),
+                                      ([50] * 100 + [16000, 3, 8000], 3, 45), ([20000] + [40] * 70, 2, 12)])
+def test_a_long_cache_among_short_ones(dtype, packed, lens, G, W):
+    """Pieces of units of very different lengths, listed in the arguments and in the workspace."""
+    check(lens=lens, G=G, W=W, D=128 if G == 4 else 64, dtype=dtype, packed=packed, seed=len(lens))
+
+
+@pytest.mark.parametrize("dtype,packed", CACHES)
 @pytest.mark.parametrize("lens,G,W,counts", [([9000], 4, 40, True), ([5000, 700], 4, 70, False), ([12000] * 2, 5, 9, True)])
 def test_many_query_rows_on_long_caches(dtype, packed, lens, G, W, counts):
     """Pieces of the wide kernel's reaches, in blocks of 128 and 256 rows."""
