@@ -580,4 +580,19 @@ hipError_t launch_per_query_norms_f32(const UnitTable& tab, const Shape& sh, con
 hipError_t launch_decode(const UnitTable& tab, const Shape& sh, kvs_dtype dt, const void* Q, const void* K,
                          const void* V, const int32_t* counts, float* part, float* out, hipStream_t stream);
 
+// The last i < n with first(i) <= x, where first ascends and first(0) <= x.  Looks at as many as a wavefront has lanes at once,
+// all of which go together.
+template <typename F>
+__device__ __forceinline__ int last_not_above(int n, int x, F&& first) {
+  const int lane = threadIdx.x % kWave;
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + kWave - 1) / kWave, i = lane * step;
+    const int k = __popcll(__ballot(i < n && first(lo + i) <= x)) - 1;
+    lo += k * step;
+    n = n - k * step < step ? n - k * step : step;
+  }
+  return lo;
+}
+
 }  // namespace kvs

@@ -5,7 +5,7 @@
 // of a block of 32 exchange the largest magnitude by lane moves.  One row per thread: the wavefronts of many short workgroups
 // have as much on its way as memory takes, and several rows per thread are slower (256 caches of 4096 bf16 rows of 128 channels,
 // 679 MB: packing 116 us, 5.8 TB/s, 120 with two rows and 124 with four; unpacking 120; 100 fp32 caches of unequal lengths up to
-// 9000 rows of 64 channels 66 and 64 us, with four rows 68 and 96).
+// 9000 rows of 64 channels 65 and 68 us).
 #include "kvs_fp4.h"
 #include "kvs_pack.h"
 
@@ -13,8 +13,7 @@ namespace kvs {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kEach = 8;                 // values per thread and row
-template <int D> constexpr int rows_per_group() { return kThreads * kEach / D; }
+constexpr int kEach = kPackValues / kThreads;      // values per thread and row
 
 template <typename T> struct Eight;
 template <> struct Eight<uint16_t> {
@@ -58,12 +57,26 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[8], uint32_t& scale)
   return codes;
 }
 
+// The thread's unit and row.
+template <int D, typename Tab>
+__device__ __forceinline__ int place(const Tab& tab, RowMove& mv) {
+  int group = blockIdx.x;
+  if constexpr (Tab::kListed) {
+    const int i = tab.unit_of(group);
+    mv = tab.unit(i);
+    group -= tab.before[i];
+  } else {
+    mv = tab.unit(blockIdx.y);
+  }
+  return group * (kPackValues / D) + (int)threadIdx.x * kEach / D;
+}
+
 template <typename T, int D, typename Tab>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const Tab tab, const T* __restrict__ K, const T* __restrict__ V,
                                                         uint8_t* __restrict__ kc, uint8_t* __restrict__ ks,
                                                         uint8_t* __restrict__ vc, uint8_t* __restrict__ vs) {
-  const RowMove mv = tab.unit(blockIdx.y);
-  const int row = (int)blockIdx.x * rows_per_group<D>() + (int)threadIdx.x * kEach / D;
+  RowMove mv;
+  const int row = place<D>(tab, mv);
   const int ch = (int)threadIdx.x * kEach % D;
   if (row >= mv.len) return;               // (a row's threads go together)
   const size_t from = ((size_t)mv.src + row) * D + ch, to = ((size_t)mv.dst + row) * D + ch;
@@ -88,8 +101,8 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const Tab tab, const u
                                                           const uint8_t* __restrict__ ks, const uint8_t* __restrict__ vc,
                                                           const uint8_t* __restrict__ vs, T* __restrict__ K,
                                                           T* __restrict__ V) {
-  const RowMove mv = tab.unit(blockIdx.y);
-  const int row = (int)blockIdx.x * rows_per_group<D>() + (int)threadIdx.x * kEach / D;
+  RowMove mv;
+  const int row = place<D>(tab, mv);
   const int ch = (int)threadIdx.x * kEach % D;
   if (row >= mv.len) return;
   const size_t from = ((size_t)mv.src + row) * D + ch, to = ((size_t)mv.dst + row) * D + ch;
@@ -104,42 +117,41 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const Tab tab, const u
   }
 }
 
-// f(table, type, dimension): a launch with the table, element type and head dimension at hand.
+// f(table, type, dimension, grid): a launch with the table, element type and head dimension at hand.
 template <typename F>
 hipError_t with_types(const EqualMoves* equal, const ListedMoves* listed, kvs_dtype dt, int D, F&& f) {
-  auto typed = [&](const auto& tab) {
+  auto typed = [&](const auto& tab, dim3 grid) {
     if (dt == KVS_F32) {
-      if (D == 64) f(tab, (float*)nullptr, std::integral_constant<int, 64>{});
-      else f(tab, (float*)nullptr, std::integral_constant<int, 128>{});
+      if (D == 64) f(tab, (float*)nullptr, std::integral_constant<int, 64>{}, grid);
+      else f(tab, (float*)nullptr, std::integral_constant<int, 128>{}, grid);
     } else {
-      if (D == 64) f(tab, (uint16_t*)nullptr, std::integral_constant<int, 64>{});
-      else f(tab, (uint16_t*)nullptr, std::integral_constant<int, 128>{});
+      if (D == 64) f(tab, (uint16_t*)nullptr, std::integral_constant<int, 64>{}, grid);
+      else f(tab, (uint16_t*)nullptr, std::integral_constant<int, 128>{}, grid);
     }
   };
-  if (equal) typed(*equal);
-  else typed(*listed);
+  const int per = kPackValues / D;
+  if (equal) typed(*equal, dim3((equal->first.len + per - 1) / per, equal->n));
+  else typed(*listed, dim3(listed->groups));
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_pack(const EqualMoves* equal, const ListedMoves* listed, int n_units, int longest, kvs_dtype dt, int D,
-                       const void* K, const void* V, const PackedRange& to, hipStream_t stream) {
-  return with_types(equal, listed, dt, D, [&](const auto& tab, auto* t, auto d) {
+hipError_t launch_pack(const EqualMoves* equal, const ListedMoves* listed, kvs_dtype dt, int D, const void* K, const void* V,
+                       const PackedRange& to, hipStream_t stream) {
+  return with_types(equal, listed, dt, D, [&](const auto& tab, auto* t, auto d, dim3 grid) {
     typedef std::remove_pointer_t<decltype(t)> T;
-    constexpr int DIM = decltype(d)::value, per = rows_per_group<DIM>();
-    hipLaunchKernelGGL((pack_kernel<T, DIM, std::decay_t<decltype(tab)>>), dim3((longest + per - 1) / per, n_units),
-                       dim3(kThreads), 0, stream, tab, (const T*)K, (const T*)V, to.kc, to.ks, to.vc, to.vs);
+    hipLaunchKernelGGL((pack_kernel<T, decltype(d)::value, std::decay_t<decltype(tab)>>), grid, dim3(kThreads), 0, stream, tab,
+                       (const T*)K, (const T*)V, to.kc, to.ks, to.vc, to.vs);
   });
 }
 
-hipError_t launch_unpack(const EqualMoves* equal, const ListedMoves* listed, int n_units, int longest, kvs_dtype dt, int D,
-                         const PackedRange& from, void* K, void* V, hipStream_t stream) {
-  return with_types(equal, listed, dt, D, [&](const auto& tab, auto* t, auto d) {
+hipError_t launch_unpack(const EqualMoves* equal, const ListedMoves* listed, kvs_dtype dt, int D, const PackedRange& from, void* K,
+                         void* V, hipStream_t stream) {
+  return with_types(equal, listed, dt, D, [&](const auto& tab, auto* t, auto d, dim3 grid) {
     typedef std::remove_pointer_t<decltype(t)> T;
-    constexpr int DIM = decltype(d)::value, per = rows_per_group<DIM>();
-    hipLaunchKernelGGL((unpack_kernel<T, DIM, std::decay_t<decltype(tab)>>), dim3((longest + per - 1) / per, n_units),
-                       dim3(kThreads), 0, stream, tab, from.kc, from.ks, from.vc, from.vs, (T*)K, (T*)V);
+    hipLaunchKernelGGL((unpack_kernel<T, decltype(d)::value, std::decay_t<decltype(tab)>>), grid, dim3(kThreads), 0, stream, tab,
+                       from.kc, from.ks, from.vc, from.vs, (T*)K, (T*)V);
   });
 }
 

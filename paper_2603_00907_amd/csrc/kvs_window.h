@@ -114,20 +114,10 @@ struct ListedUnits {
     const UnitEntry e = entry(i);
     return {e.in_row, e.len, first + i, e.before};
   }
-  // The unit of piece f (0 <= f < pieces), by a search that looks at 64 units at once.  A grid as wide for every unit as the longest
-  // needs spends 2 ns on each workgroup that finds nothing to do (one token on 999 caches of 100 rows and one of 131072: 60 us, in
-  // such a grid 589).
+  // The unit of piece f (0 <= f < pieces).  (A grid as wide for every unit as the longest needs spends 2 ns on each workgroup that
+  // finds nothing to do: one token on 999 caches of 100 rows and one of 131072: 60 us, in such a grid 589.)
   __device__ __forceinline__ int unit_of(int f) const {
-    const int lane = threadIdx.x % kWave;
-    int lo = 0, count = n;
-    while (count > 1) {
-      const int step = (count + kWave - 1) / kWave, i = lane * step;
-      const bool not_after = i < count && (ext != nullptr ? ext[lo + i].before : u[lo + i].before) - before <= f;
-      const int k = __popcll(__ballot(not_after)) - 1;
-      lo += k * step;
-      count = min(step, count - k * step);
-    }
-    return lo;
+    return last_not_above(n, f + before, [&](int i) { return ext != nullptr ? ext[i].before : u[i].before; });
   }
 };
 

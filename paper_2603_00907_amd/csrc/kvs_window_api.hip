@@ -2,6 +2,7 @@
 // between the two kinds of cache (kvs_pack, kvs_unpack): argument checks, workspace, unit tables, launches.  Everything that
 // can fail because of the arguments fails before the first launch.  Nothing here throws.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -17,7 +18,7 @@ namespace {
 
 constexpr long long kMostRow = 1ll << 48;      // rows that a cache may have: byte offsets stay far below 2^63
 constexpr long long kComputeUnits = 256;
-constexpr long long kMostGroups = 1ll << 22;   // workgroups of one launch (a grid has less than 2^32 threads, a workgroup up to 768)
+constexpr long long kMostGroups = 1ll << 22;   // workgroups of one launch, which have less than 2^32 threads together
 
 // The fields that every one of these calls reads.
 kvs_status check_common(const kvs_problem* p, int* elt) {
@@ -323,7 +324,7 @@ kvs_status check_disjoint(const kvs_problem* p) {
   return KVS_OK;
 }
 
-// The checks of both directions, then f(equal, listed, n_units, longest) for every launch.  rows, packed: K, V and the four
+// The checks of both directions, then f(equal, listed) for every launch.  rows, packed: K, V and the four
 // packed arrays; to_packed: which side is written.
 template <typename F>
 kvs_status convert(const kvs_problem* p, const void* K, const void* V, const PackedRange& c, bool to_packed, F&& f) {
@@ -347,10 +348,10 @@ kvs_status convert(const kvs_problem* p, const void* K, const void* V, const Pac
   if ((st = check_ranges(b.r, b.n)) != KVS_OK) return st;
 
   (void)hipGetLastError();
-  auto move = [&](int u) { return RowMove{p->in_row[u], p->out_row[u], p->len[u]}; };
+  const int per = kPackValues / p->head_dim;
   hipError_t e = hipSuccess;
   for (int first = 0, n = 0; e == hipSuccess && first < p->n_units; first += n) {
-    EqualMoves equal = {move(first), 0, 0};
+    EqualMoves equal = {{p->in_row[first], p->out_row[first], p->len[first]}, 0, 0, 1};
     n = 1;
     if (first + 1 < p->n_units) {
       equal.src_step = p->in_row[first + 1] - p->in_row[first];
@@ -361,19 +362,22 @@ kvs_status convert(const kvs_problem* p, const void* K, const void* V, const Pac
            p->out_row[first + n] - p->out_row[first + n - 1] == equal.dst_step) {
       ++n;
     }
-    const int listed_n = std::min(kListedMoves, p->n_units - first);
-    if (n >= listed_n) {                       // the longer run of the two
-      if (equal.first.len > 0) e = f(&equal, (const ListedMoves*)nullptr, n, equal.first.len);
+    if (n >= std::min(kListedMoves, p->n_units - first)) {     // the longer run of the two
+      equal.n = n;
+      if (equal.first.len > 0) e = f(&equal, (const ListedMoves*)nullptr);
       continue;
     }
-    n = listed_n;
-    ListedMoves listed;
-    int longest = 0;
-    for (int i = 0; i < kListedMoves; ++i) {
-      listed.u[i] = move(first + std::min(i, n - 1));
-      longest = std::max(longest, listed.u[i].len);
+    ListedMoves listed = {};
+    for (n = 0; n < kListedMoves && first + n < p->n_units; ++n) {
+      const int u = first + n, groups = (p->len[u] + per - 1) / per;
+      if (n > 0 && listed.groups > kMostMoveGroups - groups) break;
+      listed.u[n] = {p->in_row[u], p->out_row[u], p->len[u]};
+      listed.before[n] = listed.groups;
+      listed.groups += groups;
     }
-    if (longest > 0) e = f((const EqualMoves*)nullptr, &listed, n, longest);
+    listed.n = n;
+    for (int i = n; i < kListedMoves; ++i) listed.before[i] = INT_MAX;
+    if (listed.groups > 0) e = f((const EqualMoves*)nullptr, &listed);
   }
   return launched(e, "a conversion launch");
 }
@@ -411,16 +415,16 @@ kvs_status kvs_window_attention_packed(const kvs_problem* p, int32_t span, const
 kvs_status kvs_pack(const kvs_problem* p, const void* K, const void* V, void* K_codes, void* K_scales, void* V_codes,
                     void* V_scales, void* hip_stream) {
   const PackedRange to = {(uint8_t*)K_codes, (uint8_t*)K_scales, (uint8_t*)V_codes, (uint8_t*)V_scales};
-  return convert(p, K, V, to, /*to_packed=*/true, [&](const EqualMoves* equal, const ListedMoves* listed, int n, int longest) {
-    return launch_pack(equal, listed, n, longest, p->io_dtype, p->head_dim, K, V, to, (hipStream_t)hip_stream);
+  return convert(p, K, V, to, /*to_packed=*/true, [&](const EqualMoves* equal, const ListedMoves* listed) {
+    return launch_pack(equal, listed, p->io_dtype, p->head_dim, K, V, to, (hipStream_t)hip_stream);
   });
 }
 
 kvs_status kvs_unpack(const kvs_problem* p, const void* K_codes, const void* K_scales, const void* V_codes,
                       const void* V_scales, void* K, void* V, void* hip_stream) {
   const PackedRange from = {(uint8_t*)K_codes, (uint8_t*)K_scales, (uint8_t*)V_codes, (uint8_t*)V_scales};
-  return convert(p, K, V, from, /*to_packed=*/false, [&](const EqualMoves* equal, const ListedMoves* listed, int n, int longest) {
-    return launch_unpack(equal, listed, n, longest, p->io_dtype, p->head_dim, from, K, V, (hipStream_t)hip_stream);
+  return convert(p, K, V, from, /*to_packed=*/false, [&](const EqualMoves* equal, const ListedMoves* listed) {
+    return launch_unpack(equal, listed, p->io_dtype, p->head_dim, from, K, V, (hipStream_t)hip_stream);
   });
 }
 

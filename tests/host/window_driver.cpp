@@ -110,30 +110,37 @@ hipError_t launch_window_reduce(const EqualUnits* equal, const ListedUnits* list
 }
 
 namespace {
-hipError_t moved(const EqualMoves* equal, const ListedMoves* listed, int n, int longest) {
-  CHECK((equal != nullptr) != (listed != nullptr) && n > 0 && n <= kMostMoves && longest > 0);
-  CHECK(listed == nullptr || n <= kListedMoves);
+hipError_t moved(const EqualMoves* equal, const ListedMoves* listed, int D) {
+  CHECK((equal != nullptr) != (listed != nullptr));
+  CHECK(equal ? equal->n > 0 && equal->n <= kMostMoves && equal->first.len > 0 : listed->n > 0 && listed->n <= kListedMoves);
+  const int n = equal ? equal->n : listed->n, per = kPackValues / D;
+  int groups = 0;
   for (int i = 0; i < n; ++i) {
     const RowMove m = equal ? RowMove{equal->first.src + i * equal->src_step, equal->first.dst + i * equal->dst_step,
                                       equal->first.len}
                             : listed->u[i];
-    CHECK(m.len <= longest);
+    if (listed) {
+      CHECK(listed->before[i] == groups);
+      groups += (m.len + per - 1) / per;
+    }
     if (m.len == 0) continue;
     int u = g_done.empty() ? 0 : g_done.back() + 1;      // (in the order of the units)
     while (g_problem->len[u] == 0) ++u;
     CHECK(m.src == g_problem->in_row[u] && m.dst == g_problem->out_row[u] && m.len == g_problem->len[u]);
     g_done.push_back(u);
   }
+  if (listed) for (int i = n; i < kListedMoves; ++i) CHECK(listed->before[i] > groups);
+  if (listed) CHECK(groups > 0 && groups == listed->groups && groups < 1 << 24);
   return hipSuccess;
 }
 }  // namespace
-hipError_t launch_pack(const EqualMoves* equal, const ListedMoves* listed, int n, int longest, kvs_dtype, int, const void*,
-                       const void*, const PackedRange&, hipStream_t) {
-  return moved(equal, listed, n, longest);
+hipError_t launch_pack(const EqualMoves* equal, const ListedMoves* listed, kvs_dtype, int D, const void*, const void*,
+                       const PackedRange&, hipStream_t) {
+  return moved(equal, listed, D);
 }
-hipError_t launch_unpack(const EqualMoves* equal, const ListedMoves* listed, int n, int longest, kvs_dtype, int,
-                         const PackedRange&, void*, void*, hipStream_t) {
-  return moved(equal, listed, n, longest);
+hipError_t launch_unpack(const EqualMoves* equal, const ListedMoves* listed, kvs_dtype, int D, const PackedRange&, void*, void*,
+                         hipStream_t) {
+  return moved(equal, listed, D);
 }
 
 }  // namespace kvs
@@ -228,6 +235,9 @@ int main() {
   CHECK(attend(Call({KVS_MAX_LEN, 1, 0}, 64, 65536), 2147483647, true) == KVS_OK);
   CHECK(attend(Call(std::vector<int32_t>(100000, 1)), 0, true) == KVS_OK);
   CHECK(convert(Call(std::vector<int32_t>(200000, 2))) == KVS_OK);
+  std::vector<int32_t> longs(150, KVS_MAX_LEN);
+  for (int i = 0; i < 150; ++i) longs[i] -= i % 7;
+  CHECK(convert(Call(longs)) == KVS_OK);
 
   // refusals, each before any launch
   auto refused = [&](kvs_status want, auto&& change, int span = 0) {

@@ -141,3 +141,25 @@ def test_equal_units_of_few_rows(units, n):
             got = got.cpu().numpy().reshape(units, room, -1)
             assert (got[:, 1:1 + n] == want.reshape(units, n, -1)).all()
             assert (got[:, 0] == 0xA5).all() and (got[:, 1 + n:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("lens", [[3] * 40 + [5000, 0, 0, 17], [0] * 20 + [33] * 100 + [9000] + [0, 1] * 30, [4000, 1, 0, 70]])
+def test_long_units_among_short_ones(dtype, D, lens):
+    import torch
+    import paper_2603_00907_amd as kvs
+    rng = np.random.default_rng(len(lens))
+    rows = sum(lens)
+    K, V = rows_of(rng, rows, D, dtype), rows_of(rng, rows, D, dtype)
+    p = kvs.Problem(lens=lens, budgets=lens, group=1, window=1, head_dim=D, dtype=dtype)
+    buf, stream = packed_buffers(rows + 2, D), torch.cuda.current_stream().cuda_stream
+    kvs.kvs_pack(p, to_device(K, dtype), to_device(V, dtype), *buf, stream=stream)
+    for x, codes, scales in ((K, buf[0], buf[1]), (V, buf[2], buf[3])):
+        for got, want in zip((codes, scales), R.pack(x)):
+            got = got.cpu().numpy()
+            assert (got[:rows] == want).all() and (got[rows:] == 0xA5).all()
+    out = [torch.full((rows + 2, D), 512.0, device="cuda").to(torch_io_dtype(dtype)) for _ in range(2)]
+    kvs.kvs_unpack(p, *buf, *out, stream=stream)
+    for o, x in zip(out, (K, V)):
+        o = o.float().cpu().numpy()
+        assert (o[:rows] == R.unpack(*R.pack(x))).all() and (o[rows:] == 512).all()
