@@ -91,7 +91,6 @@ struct Cut {
     const long long times = (equal ? p->n_units : 1ll) * sh.n_blocks;
     return {s.groups * times, s.tiles * times, s.partial * times};
   }
-  long long workgroups(long long per) const { return with(per).groups; }
 };
 
 // kvs_window_rows.hip: the longest pieces that make no more workgroups than run at once, since memory bounds all of them alike and
@@ -112,11 +111,15 @@ void cut_rows(const kvs_problem* p, long long at_once, WindowShape& sh) {
   // (more units than that: whole reaches, or the longest of unequal ones cut)
   const long long limit = whole <= at_once ? at_once : cut.equal ? whole : whole + at_once;
   long long per = std::max(kLeastTiles, (cut.most + kMaxParts - 1) / kMaxParts);
-  if (cut.workgroups(per) > limit) {
+  const Cut::Sums shortest = cut.with(per);
+  if (shortest.groups > limit) {
+    // (tiles / per <= workgroups < tiles / per + whole)
     long long fits = std::max(per, cut.most);
+    if (limit > whole) fits = std::min(fits, shortest.tiles / (limit - whole) + 1);
+    per = std::max(per, (shortest.tiles + limit - 1) / limit - 1);
     while (fits - per > 1) {
       const long long mid = (per + fits) / 2;
-      if (cut.workgroups(mid) > limit) per = mid;
+      if (cut.with(mid).groups > limit) per = mid;
       else fits = mid;
     }
     per = fits;
