@@ -592,7 +592,7 @@ __device__ __forceinline__ int last_not_above(int n, int x, F&& first) {
     lo += k * step;
     n = n - k * step < step ? n - k * step : step;
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
 }  // namespace kvs

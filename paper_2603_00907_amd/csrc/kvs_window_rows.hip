@@ -254,14 +254,19 @@ __device__ __forceinline__ void store_two(T* at, float a, float b) {
   else *(uint32_t*)at = cvt_pk_bf16(a, b);
 }
 
-// Wavefronts per SIMD that the registers are allotted for: the operands of a tile and of the queries, and the accumulators.
-template <CacheKind KIND, int D, int NQ>
+// Wavefronts per SIMD that the registers are allotted for: the operands of a tile and of the queries, and the accumulators.  One
+// more would have some of them spilled (fp32 queries over rows in 4 bits of 128 channels, one token on 256 caches of 4096 rows:
+// 43.6 us with two wavefronts, 47.7 with three, with cardinalities 51 and 105; listed units with cardinalities, 32 query rows on 64
+// caches of 2250 to 9000 bf16 rows: 52 us with one, 85 with two).
+template <CacheKind KIND, int D, int NQ, bool COUNTS, typename Tab>
 constexpr int waves_per_simd() {
-  return KIND == CacheKind::kF32 && D == 128 ? (NQ == 1 ? 2 : 1) : NQ == 1 && KIND != CacheKind::kBf16 ? 3 : 2;
+  if (KIND == CacheKind::kF32 || KIND == CacheKind::kPackedF32) return (NQ == 1 ? 2 : 1) + (D == 64);
+  if (KIND == CacheKind::kBf16) return NQ == 2 && D == 128 && COUNTS && Tab::kListed ? 1 : 2;
+  return NQ == 1 ? 3 : 2;
 }
 
 template <CacheKind KIND, int D, int NQ, int WAVES, bool COUNTS, typename Tab>
-__global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, NQ>())) void window_rows_kernel(
+__global__ __launch_bounds__(WAVES * kWave, (waves_per_simd<KIND, D, NQ, COUNTS, Tab>())) void window_rows_kernel(
     const Tab tab, const WindowShape sh, const Cache cache, const void* __restrict__ Q, void* __restrict__ out,
     float* __restrict__ part) {
   typedef Rows<KIND, D> L;
@@ -667,19 +672,19 @@ template <CacheKind KIND, int D, typename Tab>
 hipError_t launch_kind(const Tab& tab, const WindowShape& sh, const Cache& cache, const void* Q, void* out, float* part,
                        hipStream_t stream) {
   const dim3 grid((unsigned)(pieces_of(tab, sh) * sh.n_blocks));
-  auto go = [&](auto nq, auto waves) {
+  auto go = [&](auto nq, auto counts, auto waves) {
     constexpr int NQ = decltype(nq)::value, WAVES = decltype(waves)::value;
-    auto counted = [&](auto counts) {
-      hipLaunchKernelGGL((window_rows_kernel<KIND, D, NQ, WAVES, decltype(counts)::value, Tab>), grid, dim3(WAVES * kWave), 0,
-                         stream, tab, sh, cache, Q, out, part);
-    };
-    if (cache.counts) counted(std::true_type{});
-    else counted(std::false_type{});
+    hipLaunchKernelGGL((window_rows_kernel<KIND, D, NQ, WAVES, decltype(counts)::value, Tab>), grid, dim3(WAVES * kWave), 0,
+                       stream, tab, sh, cache, Q, out, part);
+  };
+  auto counted = [&](auto nq, auto counts) {
+    constexpr int MANY = 4 * waves_per_simd<KIND, D, decltype(nq)::value, decltype(counts)::value, Tab>();
+    if (sh.large) go(nq, counts, std::integral_constant<int, MANY>{});
+    else go(nq, counts, std::integral_constant<int, 4>{});
   };
   auto sized = [&](auto nq) {
-    constexpr int NQ = decltype(nq)::value, MANY = 4 * waves_per_simd<KIND, D, NQ>();
-    if (sh.large) go(nq, std::integral_constant<int, MANY>{});
-    else go(nq, std::integral_constant<int, 4>{});
+    if (cache.counts) counted(nq, std::true_type{});
+    else counted(nq, std::false_type{});
   };
   if (sh.block == 16) sized(std::integral_constant<int, 1>{});
   else sized(std::integral_constant<int, 2>{});
