@@ -194,7 +194,9 @@ kvs_status make_window_plan(const kvs_problem* p, int32_t span, bool packed, Win
   // (64 channels, pieces of 22 and 65 tiles: 768 workgroups 18.9 us, 256 26.0; 16 query rows of 128 channels 27.4 and 37.8;
   // fp32 queries, which take more registers, 8 caches of 131072 rows: 49.5 with 512, 59.2 with 768).
   // The wide kernel's are one or two (see there).
-  const int per_unit = plan->wide ? (sh.D == 64 || (packed && sh.block == 128) ? 2 : 1) : !packed ? 1 : (sh.block == 16 ? 3 : 2) - (*elt == 4 && sh.D == 128);
+  int per_unit = 1;
+  if (plan->wide) per_unit = sh.D == 64 || (packed && sh.block == 128) ? 2 : 1;
+  else if (packed) per_unit = (sh.block == 16 ? 3 : 2) - (*elt == 4 && sh.D == 128);
   if (plan->wide) cut_tiles(p, kComputeUnits * per_unit, sh);
   else cut_rows(p, kComputeUnits * per_unit, sh);
   plan->equal = true;
