@@ -15,7 +15,7 @@
 // is too large (or not a number) has the largest logit looked for.  One barrier per tile: while tile j is worked on, K of tile
 // j + 2 and V of tile j + 1 travel through registers into the buffers of LDS that nobody reads.  Pieces of 16 bytes are
 // swizzled within a row of LDS so that neither kind of read meets a bank twice (no conflicts counted).
-// Measured on a prompt of 8192 tokens, 32 heads of 128 channels, causal (0.55 TFLOP): 530 to 560 us on different cards, 0.98 to
+// Measured on a prompt of 8192 tokens, 32 heads of 128 channels, causal (0.55 TFLOP): 530 to 600 us on different cards, 0.92 to
 // 1.04 PFLOP/s where a large matrix product reaches 1.29; matrix cores busy for 0.48 of the cycles.  Without memory, LDS and
 // barrier it would take 409.  Slower: the products and their exponentials one after the other with all operands read ahead
 // (576), loads straight into LDS (545; the transposing reads then wait for all of them, or have to be assembly), 64 query rows
